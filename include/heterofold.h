@@ -22,6 +22,12 @@
  *     (or hf_transfer_host    the same with both caches in host memory)
  *   hf_plan_destroy
  *
+ * A receiver then uses its cache (what the paper leaves to the receiver model's
+ * own software):
+ *   hf_cache_append           keys and values of new tokens behind the others
+ *   hf_attend                 attention of packed queries over the cache
+ *   hf_cache_read             rows of a cache as dense keys and values
+ *
  * General rules:
  *  - Every pointer prefixed d_ is device memory; h_ or unprefixed arrays
  *    documented as "host" are host memory.  The library allocates no device
@@ -448,6 +454,163 @@ hf_status hf_recolor_fit(hf_dtype dtype, int64_t N, int32_t d_S, int32_t d_R, co
                          const void* d_Y, const float* d_w, float reg, void* d_W_out,
                          float* d_b_out, float* h_r_out, int32_t* h_iters_out,
                          void* d_workspace, size_t workspace_bytes, hf_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Using a cache: append, read, attend
+ * ------------------------------------------------------------------------- */
+
+/* How a cache holds keys and values. */
+typedef enum {
+  HF_CACHE_BF16 = 0,
+  HF_CACHE_F32 = 1,
+  /* 4 bits and a scale for every 32 channels (4.5 bits a value).  A group of 32
+     channels y of a row and head has a = max |y|, scale = a / 7 rounded to 5
+     significant bits (half up; 0 where a / 7 is below 2^-100), and
+     code = clamp(rint(y / scale), -7, 7) + 8; its values are
+     scale * (code - 8), which have at most 8 significant bits: bf16 holds them
+     exactly.  A group with an infinity or a NaN holds NaN in all its channels.
+     d_k and d_v: uint8 [H][rows][D / 2], channel c = 32 g + 4 j + i
+     (g < D / 32, j < 8, i < 4) in nibble (D / 8) j + 4 g + i (low nibble of a
+     byte first); d_k_scale and d_v_scale: bf16 [H][rows][D / 32]. */
+  HF_CACHE_Q4 = 2
+} hf_cache_kind;
+
+/* The keys and values of one layer for n_seq sequences.  A zero-initialised
+   descriptor leaves optional fields off.  The layer l of a receiver cache of
+   hf_plan_desc is d_k = receiver_kv + (2 l) rows H D, d_v = receiver_kv +
+   (2 l + 1) rows H D elements. */
+typedef struct {
+  hf_cache_kind kind;
+  int32_t H, D;           /* KV heads, head width: 32, 64, 96, 128 or 256 (Q4: 64, 128, 256) */
+  int32_t n_seq;          /* sequences, 1 .. 1024 */
+  int64_t rows;           /* rows of the buffers (paged: n_blocks * block_size), < 2^31 */
+  void* d_k;              /* bf16, fp32: [rows][H][D] unless strides are given; 16-byte aligned */
+  void* d_v;
+  void* d_k_scale;        /* Q4 only; aligned to D / 16 bytes */
+  void* d_v_scale;
+  /* bf16 and fp32: elements from a row to the next and from a head to the
+     next, multiples of 16 bytes (0: H D and D), for keys and values that lie
+     in a larger tensor. */
+  int64_t row_stride, head_stride;
+  /* Paged: row t of sequence s is row d_block_table[s * max_blocks_per_seq +
+     t / block_size] * block_size + t % block_size.  Contiguous
+     (d_block_table NULL): row d_row0[s] + t. */
+  const int32_t* d_block_table; /* device int32[n_seq][max_blocks_per_seq] */
+  int32_t block_size;
+  int32_t max_blocks_per_seq;
+  const int32_t* d_row0;  /* device int32[n_seq], or NULL for 0 (n_seq 1) */
+  /* device int32 the calls set HF_CHECK_* bits in, or NULL: BAD_OFFSETS
+     (token pointers that decrease or pass n_tok), CAPACITY (rows outside the
+     cache, positions outside the rotation table), BAD_BLOCK.  Such rows are
+     not written, and read as zeros. */
+  int32_t* d_status;
+} hf_cache;
+
+/* New tokens of a cache's sequences.  Tokens [d_tok_ptr[s], d_tok_ptr[s+1])
+   of the packed arrays belong to sequence s and take its rows d_start[s],
+   d_start[s] + 1, ...  Strides are in elements, multiples of 16 bytes (0:
+   dense [n_tok][heads][D]); pointers are 16-byte aligned. */
+typedef struct {
+  hf_dtype dtype;              /* of k, v and q; the cache's own unless it is Q4 */
+  int32_t n_tok;               /* d_tok_ptr[n_seq] */
+  const int32_t* d_tok_ptr;    /* device int32[n_seq+1] */
+  const int32_t* d_start;      /* device int32[n_seq] */
+  const void* d_k;
+  const void* d_v;
+  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  /* Optional: the tokens' queries, normed and rotated like the keys into
+     d_q_out (d_q itself, or not overlapping it), the same strides. */
+  int32_t H_q;
+  const void* d_q;
+  void* d_q_out;
+  int64_t q_row_stride, q_head_stride;
+  /* Optional rotation of keys and queries, rotate-half pairs (i, i + D/2):
+     cos and sin of every position [rope_len][D/2][2] (hf_rope_table).  The
+     position of a token is its row in the sequence plus d_pos0[s]. */
+  const float* d_rope;
+  int32_t rope_len;
+  const int32_t* d_pos0;       /* device int32[n_seq], or NULL for 0 */
+  /* Optional RMS norms before the rotation, device float[D] weights. */
+  const float* d_k_norm;
+  const float* d_q_norm;
+  float eps;
+} hf_append_desc;
+
+/*
+ * hf_rope_table — cos and sin of pos * inv_freq_i, fp32 [n_pos][D/2][2], at
+ * positions pos0 .. pos0 + n_pos - 1 (below 2^24), with hf_transfer's angle
+ * arithmetic: inv_freq from the host table, or fp32(theta^(-2i/D)) where it is
+ * NULL.  Asynchronous.
+ */
+hf_status hf_rope_table(int32_t D, double theta, const float* h_inv_freq, int32_t pos0,
+                        int32_t n_pos, float* d_table, hf_stream_t stream);
+
+/*
+ * hf_cache_append — writes the tokens' keys (normed and rotated where asked)
+ * and values into their cache rows, rounded once to what the cache holds; rows
+ * of different tokens must differ.  The rotation multiplies and adds in fp32
+ * with a rounding each.  One launch; n_tok 0 does nothing.  Without norm and
+ * rotation and with a transferred cache as k and v it packs that cache.
+ */
+hf_status hf_cache_append(const hf_cache* cache, const hf_append_desc* desc, hf_stream_t stream);
+
+/* Packed rows to be read: rows d_start[s] .. of sequence s as tokens
+   [d_tok_ptr[s], d_tok_ptr[s+1]) of dense [n_tok][H][D] arrays. */
+typedef struct {
+  hf_dtype dtype;              /* of k and v; the cache's own unless it is Q4 */
+  int32_t n_tok;
+  const int32_t* d_tok_ptr;    /* device int32[n_seq+1] */
+  const int32_t* d_start;      /* device int32[n_seq] */
+  void* d_k;                   /* out, 16-byte aligned */
+  void* d_v;
+  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride; /* as above */
+} hf_read_desc;
+
+/*
+ * hf_cache_read — the values that the cache holds, in dense rows: a 4-bit
+ * cache's for a transfer that reads them as its sender cache, for instance.
+ * One launch; n_tok 0 does nothing.
+ */
+hf_status hf_cache_read(const hf_cache* cache, const hf_read_desc* desc, hf_stream_t stream);
+
+/* Attention of packed queries over a cache.  Queries [d_q_ptr[s],
+   d_q_ptr[s+1]) belong to sequence s, whose cache holds d_kv_len[s] rows, the
+   queries' own among them.  Query head h reads KV head h / (H_q / H). */
+typedef struct {
+  hf_dtype dtype;              /* of q and out; the cache's own unless it is Q4 */
+  int32_t H_q;                 /* query heads, a multiple of H */
+  int32_t n_tok;               /* d_q_ptr[n_seq] */
+  const int32_t* d_q_ptr;      /* device int32[n_seq+1] */
+  const int32_t* d_kv_len;     /* device int32[n_seq] */
+  /* Upper bounds of the sequences' query tokens and cache rows, from which
+     kernels and splits are chosen (and nothing else: a wrong bound costs
+     speed). */
+  int32_t max_q_len, max_kv_len;
+  /* 1: query i of n sees cache rows up to kv_len - n + i (the last query sees
+     all); 0: every row.  A query that sees no row gives zeros. */
+  int32_t causal;
+  float scale;                 /* of q . k; 0: 1 / sqrt(D) */
+  const void* d_q;             /* [n_tok][H_q][D] unless strides are given; 16-byte aligned */
+  void* d_out;                 /* like d_q */
+  int64_t q_row_stride, q_head_stride, out_row_stride, out_head_stride;
+  float* d_lse;                /* optional float[n_tok][H_q]: log of the sum of exp(scale q . k);
+                                  -inf where nothing is seen */
+} hf_attend_desc;
+
+/*
+ * hf_attend — out = softmax(scale q k^T) v per query and head, softmax in fp32,
+ * rounded once to dtype.  d_workspace: hf_attend_workspace_size bytes, enough
+ * for every call on such a cache, 256-byte aligned; its first HF_ATTEND_ZEROED
+ * bytes must be zero before the first call and are zero after every call; one
+ * call at a time may use it.  At most two launches; n_tok 0 does nothing.
+ * A non-finite value in a row that a query sees reaches its output as it does in
+ * fp32 sums; one in a row past kv_len never does, and one in a row that a causal
+ * query does not see may, where another query of its call sees that row.
+ */
+#define HF_ATTEND_ZEROED 65536
+hf_status hf_attend_workspace_size(const hf_cache* cache, size_t* bytes);
+hf_status hf_attend(const hf_cache* cache, const hf_attend_desc* desc, void* d_workspace,
+                    size_t workspace_bytes, hf_stream_t stream);
 
 const char* hf_status_string(hf_status status);
 const char* hf_last_error(void);

@@ -2,7 +2,8 @@
 
 Modules:
   binding   ctypes binding of include/heterofold.h (libheterofold.so)
-  pipeline  TransferJob: torch-allocated buffers + the ABI calls of a transfer
+  pipeline  TransferJob: torch-allocated buffers + the ABI calls of a transfer;
+            KVCache: a receiver's cache, appended to, read and attended over
   workloads seeded synthetic inputs shaped like the paper's model pairs
   build     nvcc build of libheterofold.so (in-tree)
 

@@ -28,6 +28,8 @@ HF_ERR_WORKSPACE = 6
 ALIGN_MODES = {"ta": 0, "overlap_mean": 1, "same_index": 2}
 LAYER_MODES = {"paper3": 0, "interp": 1, "explicit": 2}
 DTYPES = {"bf16": 0, "f32": 1}
+CACHE_KINDS = {"bf16": 0, "f32": 1, "q4": 2}
+ATTEND_ZEROED = 65536
 
 CHECK_BITS = {
     0x01: "HF_CHECK_BAD_OFFSETS", 0x02: "HF_CHECK_BAD_COLUMN", 0x04: "HF_CHECK_BAD_ROW",
@@ -39,7 +41,8 @@ EXPORTED = ("hf_align_build", "hf_plan_workspace_size", "hf_plan_create", "hf_tr
             "hf_plan_destroy", "hf_plan_device_status", "hf_plan_distinct_rows",
             "hf_status_string", "hf_last_error", "hf_transfer_noalloc", "hf_transfer_host",
             "hf_transfer_batch", "hf_fold", "hf_recolor_workspace_size", "hf_recolor_fit",
-            "hf_debug_transfer_stalled", "hf_debug_matmul_workspace_size",
+            "hf_rope_table", "hf_cache_append", "hf_cache_read", "hf_attend_workspace_size",
+            "hf_attend", "hf_debug_transfer_stalled", "hf_debug_matmul_workspace_size",
             "hf_debug_matmul_f32")
 
 _p = ctypes.c_void_p
@@ -70,6 +73,56 @@ class PlanDesc(ctypes.Structure):
         ("h_seg_layer", _i32p), ("h_seg_w", _f32p),
         ("round_built_operands", ctypes.c_int32),
         ("pool_before_map", ctypes.c_int32),
+    ]
+
+
+class CacheDesc(ctypes.Structure):
+    """Mirror of hf_cache."""
+    _fields_ = [
+        ("kind", ctypes.c_int), ("H", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("n_seq", ctypes.c_int32), ("rows", ctypes.c_int64),
+        ("d_k", _p), ("d_v", _p), ("d_k_scale", _p), ("d_v_scale", _p),
+        ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+        ("d_block_table", _p), ("block_size", ctypes.c_int32),
+        ("max_blocks_per_seq", ctypes.c_int32), ("d_row0", _p), ("d_status", _p),
+    ]
+
+
+class AppendDesc(ctypes.Structure):
+    """Mirror of hf_append_desc."""
+    _fields_ = [
+        ("dtype", ctypes.c_int), ("n_tok", ctypes.c_int32),
+        ("d_tok_ptr", _p), ("d_start", _p), ("d_k", _p), ("d_v", _p),
+        ("k_row_stride", ctypes.c_int64), ("k_head_stride", ctypes.c_int64),
+        ("v_row_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64),
+        ("H_q", ctypes.c_int32), ("d_q", _p), ("d_q_out", _p),
+        ("q_row_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+        ("d_rope", _p), ("rope_len", ctypes.c_int32), ("d_pos0", _p),
+        ("d_k_norm", _p), ("d_q_norm", _p), ("eps", ctypes.c_float),
+    ]
+
+
+class ReadDesc(ctypes.Structure):
+    """Mirror of hf_read_desc."""
+    _fields_ = [
+        ("dtype", ctypes.c_int), ("n_tok", ctypes.c_int32),
+        ("d_tok_ptr", _p), ("d_start", _p), ("d_k", _p), ("d_v", _p),
+        ("k_row_stride", ctypes.c_int64), ("k_head_stride", ctypes.c_int64),
+        ("v_row_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64),
+    ]
+
+
+class AttendDesc(ctypes.Structure):
+    """Mirror of hf_attend_desc."""
+    _fields_ = [
+        ("dtype", ctypes.c_int), ("H_q", ctypes.c_int32), ("n_tok", ctypes.c_int32),
+        ("d_q_ptr", _p), ("d_kv_len", _p),
+        ("max_q_len", ctypes.c_int32), ("max_kv_len", ctypes.c_int32),
+        ("causal", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("d_q", _p), ("d_out", _p),
+        ("q_row_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+        ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+        ("d_lse", _p),
     ]
 
 
@@ -125,12 +178,22 @@ def lib() -> ctypes.CDLL:
                                           ctypes.c_int64, ctypes.c_int64, ctypes.c_float, _p,
                                           ctypes.c_int64, _p, ctypes.c_size_t, _i32p, _p]
         L.hf_debug_matmul_f32.restype = ctypes.c_int
+        L.hf_rope_table.argtypes = [ctypes.c_int32, ctypes.c_double, _f32p, ctypes.c_int32,
+                                    ctypes.c_int32, _p, _p]
+        L.hf_cache_append.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(AppendDesc), _p]
+        L.hf_cache_read.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(ReadDesc), _p]
+        L.hf_attend_workspace_size.argtypes = [ctypes.POINTER(CacheDesc),
+                                               ctypes.POINTER(ctypes.c_size_t)]
+        L.hf_attend.argtypes = [ctypes.POINTER(CacheDesc), ctypes.POINTER(AttendDesc), _p,
+                                ctypes.c_size_t, _p]
         L.hf_status_string.argtypes = [ctypes.c_int]
         L.hf_status_string.restype = ctypes.c_char_p
         L.hf_last_error.argtypes = []
         L.hf_last_error.restype = ctypes.c_char_p
         for name in ("hf_align_build", "hf_plan_workspace_size", "hf_plan_create", "hf_transfer",
-                     "hf_plan_destroy", "hf_plan_device_status", "hf_plan_distinct_rows"):
+                     "hf_plan_destroy", "hf_plan_device_status", "hf_plan_distinct_rows",
+                     "hf_rope_table", "hf_cache_append", "hf_cache_read",
+                     "hf_attend_workspace_size", "hf_attend"):
             getattr(L, name).restype = ctypes.c_int
         _LIB = L
     return _LIB
@@ -332,6 +395,41 @@ def recolor_fit(dtype: str, X, Y, w, W_out, b_out, workspace, reg: float = 0.0,
                                 its, _dptr(workspace), nbytes, _stream(stream)),
            "hf_recolor_fit")
     return (float(r.value), list(its)) if return_iters else float(r.value)
+
+
+def rope_table(D: int, table, theta: float = 0.0, inv_freq=None, pos0: int = 0,
+               stream=None) -> None:
+    """hf_rope_table: cos and sin of positions pos0 .. into table fp32 [n_pos, D/2, 2]."""
+    f = None if inv_freq is None else _host_f32(inv_freq)
+    _check(lib().hf_rope_table(int(D), float(theta), _f32_or_null(f), int(pos0),
+                               int(table.shape[0]), _dptr(table), _stream(stream)),
+           "hf_rope_table")
+
+
+def cache_append(cache: CacheDesc, desc: AppendDesc, stream=None) -> None:
+    _check(lib().hf_cache_append(ctypes.byref(cache), ctypes.byref(desc), _stream(stream)),
+           "hf_cache_append")
+
+
+def cache_read(cache: CacheDesc, desc: ReadDesc, stream=None) -> None:
+    _check(lib().hf_cache_read(ctypes.byref(cache), ctypes.byref(desc), _stream(stream)),
+           "hf_cache_read")
+
+
+def attend_workspace_size(cache: CacheDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().hf_attend_workspace_size(ctypes.byref(cache), ctypes.byref(n)),
+           "hf_attend_workspace_size")
+    return int(n.value)
+
+
+def attend(cache: CacheDesc, desc: AttendDesc, workspace, workspace_bytes=None,
+           stream=None) -> None:
+    """hf_attend; workspace_bytes None: the workspace tensor's bytes."""
+    if workspace_bytes is None:
+        workspace_bytes = int(workspace.numel() * workspace.element_size())
+    _check(lib().hf_attend(ctypes.byref(cache), ctypes.byref(desc), _dptr(workspace),
+                           workspace_bytes, _stream(stream)), "hf_attend")
 
 
 def transfer_noalloc(desc: Desc, sender_kv, receiver_kv, stream=None) -> None:

@@ -1,0 +1,336 @@
+// Attention of packed queries over a receiver's cache: entry points, the choice
+// of a kernel, the form for every type and width, and the joining of parts.
+//
+//   o_i = sum_{j < limit_i} exp(scale q_i . k_j) v_j / sum_{j < limit_i} exp(scale q_i . k_j)
+//
+// attend_general_kernel is fp32 arithmetic throughout: fp32 caches and queries
+// (which tensor-core products would round) and the head widths that the other
+// kernels do not take.  A block of 128 threads holds 32 flattened query rows,
+// four threads a row, and walks the keys 32 at a time through shared memory with
+// a running maximum and sum.  Bound by shared-memory reads: four FMA of scores
+// take a 16-byte read of keys.
+#include <algorithm>
+#include <cmath>
+#include <string>
+
+#include "hf_attend.cuh"
+
+namespace hf {
+namespace {
+
+constexpr int kRows = 32, kKeys = 32, kThreads = 128;
+
+template <int D>
+constexpr size_t general_smem() {
+  return sizeof(float) * ((kRows + kKeys) * (D + 4) + kKeys * D + kRows * (kKeys + 1)) + sizeof(int) * kKeys;
+}
+
+// Eight channels of a row and head, chunk c, in fp32.
+template <typename T>
+__device__ __forceinline__ void load_chunk(const T* p, float* x) {
+  if constexpr (sizeof(T) == 2) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  } else {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  }
+}
+template <typename T, int KIND, int D>
+__device__ __forceinline__ void load_cache_chunk(const CacheArgs& C, bool value, int row, int h, int c, float* x) {
+  if constexpr (KIND == HF_CACHE_Q4) {
+    const int64_t at = static_cast<int64_t>(h) * C.rows + row;
+    const int g = c / 4, m = c % 4;
+    const uint16_t* codes = reinterpret_cast<const uint16_t*>((value ? C.v : C.k) + at * (D / 2)) + (D / 32) * 2 * m + g;
+    const uint16_t s16 = reinterpret_cast<const uint16_t*>((value ? C.vs : C.ks) + at * (D / 16))[g];
+    const float s = __uint_as_float(static_cast<uint32_t>(s16) << 16);
+    const uint32_t w = codes[0] | static_cast<uint32_t>(codes[D / 32]) << 16;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = s * static_cast<float>(static_cast<int>((w >> (4 * e)) & 15u) - 8);
+  } else {
+    load_chunk(reinterpret_cast<const T*>(value ? C.v : C.k) + row * C.row_stride + h * C.head_stride + 8 * c, x);
+  }
+}
+
+template <typename T, int KIND, int D>
+__global__ void __launch_bounds__(kThreads) attend_general_kernel(const CacheArgs C, const AttendArgs A, int ns) {
+  extern __shared__ __align__(16) float smem_f[];
+  float* sQ = smem_f;
+  float* sK = sQ + kRows * (D + 4);
+  float* sV = sK + kKeys * (D + 4);
+  float* sP = sV + kKeys * D;
+  int* sRow = reinterpret_cast<int*>(sP + kRows * (kKeys + 1));
+  const TilePlace at = find_tile(C, A, kRows, blockIdx.x);
+  if (at.seq >= C.n_seq) return;
+  const SeqSpan span = seq_span(C, A, at.seq);
+  const int h = blockIdx.y, sp = blockIdx.z;
+  const int r0 = at.at * kRows;
+  const int n_rows = static_cast<int>(min(static_cast<int64_t>(kRows), static_cast<int64_t>(span.n) * A.G - r0));
+  const int r = threadIdx.x >> 2, c4 = threadIdx.x & 3;
+
+  for (int i = threadIdx.x; i < kRows * (D / 8); i += kThreads) {
+    const int row = i / (D / 8), c = i % (D / 8);
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (row < n_rows) {
+      const int rr = r0 + row;
+      const int64_t tok = span.first + rr / A.G;
+      load_chunk(reinterpret_cast<const T*>(A.q) + tok * A.q_row + (h * A.G + rr % A.G) * A.q_head + 8 * c, x);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sQ[row * (D + 4) + 8 * c + e] = x[e];
+  }
+  const int last = seen(span, A.causal, (r0 + n_rows - 1) / A.G);
+  const int per = ((last + ns - 1) / ns + kKeys - 1) / kKeys * kKeys;
+  const int k0 = min(static_cast<int64_t>(sp) * per, static_cast<int64_t>(last));
+  const int k1 = min(static_cast<int64_t>(k0) + per, static_cast<int64_t>(last));
+  const int mine = r < n_rows ? min(seen(span, A.causal, (r0 + r) / A.G), k1) : 0;
+
+  float acc[D / 4], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 4; ++i) acc[i] = 0.f;
+  for (int kb = k0; kb < k1; kb += kKeys) {
+    __syncthreads();
+    if (threadIdx.x < kKeys) sRow[threadIdx.x] = kb + threadIdx.x < k1 ? cache_row(C, at.seq, kb + threadIdx.x) : -1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * kKeys * (D / 8); i += kThreads) {
+      const bool value = i >= kKeys * (D / 8);
+      const int j = value ? i - kKeys * (D / 8) : i;
+      const int key = j / (D / 8), c = j % (D / 8);
+      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (sRow[key] >= 0) load_cache_chunk<T, KIND, D>(C, value, sRow[key], h, c, x);
+      float* dst = value ? sV + key * D + 8 * c : sK + key * (D + 4) + 8 * c;
+      reinterpret_cast<float4*>(dst)[0] = make_float4(x[0], x[1], x[2], x[3]);
+      reinterpret_cast<float4*>(dst)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    }
+    __syncthreads();
+    float s[kKeys / 4];
+#pragma unroll
+    for (int i = 0; i < kKeys / 4; ++i) s[i] = 0.f;
+#pragma unroll 4
+    for (int d = 0; d < D; d += 4) {
+      const float4 q = *reinterpret_cast<const float4*>(sQ + r * (D + 4) + d);
+#pragma unroll
+      for (int i = 0; i < kKeys / 4; ++i) {
+        const float4 k = *reinterpret_cast<const float4*>(sK + (c4 + 4 * i) * (D + 4) + d);
+        s[i] = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, fmaf(q.w, k.w, s[i]))));
+      }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kKeys / 4; ++i) {
+      s[i] = kb + c4 + 4 * i < mine ? s[i] * A.scale_log2 : -INFINITY;
+      // a NaN score has to stay one: it reaches the sum below
+      top = fmaxf(top, s[i]);
+    }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const float m_new = fmaxf(m, top);
+    const float base = m_new == -INFINITY ? 0.f : m_new;
+    const float fix = exp2f(m - base);
+    m = m_new;
+    l *= fix;
+#pragma unroll
+    for (int i = 0; i < D / 4; ++i) acc[i] *= fix;
+#pragma unroll
+    for (int i = 0; i < kKeys / 4; ++i) {
+      const float p = exp2f(s[i] - base);
+      l += p;
+      sP[r * (kKeys + 1) + c4 + 4 * i] = p;
+    }
+    __syncwarp();
+    const int keys = min(kKeys, mine - kb);  // what this row does not see adds nothing, whatever it holds
+    for (int key = 0; key < keys; ++key) {
+      const float p = sP[r * (kKeys + 1) + key];
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) {
+        const float4 v = *reinterpret_cast<const float4*>(sV + key * D + 16 * j + 4 * c4);
+        acc[4 * j] = fmaf(p, v.x, acc[4 * j]);
+        acc[4 * j + 1] = fmaf(p, v.y, acc[4 * j + 1]);
+        acc[4 * j + 2] = fmaf(p, v.z, acc[4 * j + 2]);
+        acc[4 * j + 3] = fmaf(p, v.w, acc[4 * j + 3]);
+      }
+    }
+  }
+  l += __shfl_xor_sync(0xffffffffu, l, 1);
+  l += __shfl_xor_sync(0xffffffffu, l, 2);
+  if (r >= n_rows) return;
+  const int rr = r0 + r;
+  const int64_t tok = span.first + rr / A.G;
+  const int hq = h * A.G + rr % A.G;
+  if (ns > 1) {
+    const int64_t slot = (static_cast<int64_t>(sp) * A.n_tok + tok) * A.H_q + hq;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j)
+      *reinterpret_cast<float4*>(A.part_o + slot * D + 16 * j + 4 * c4) =
+          make_float4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
+    if (c4 == 0) A.part_ml[slot] = make_float2(m, l);
+    return;
+  }
+  T* dst = reinterpret_cast<T*>(A.out) + tok * A.o_row + hq * A.o_head;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dst[16 * j + 4 * c4 + e] = from_float<T>(acc[4 * j + e] * inv);
+  if (A.lse && c4 == 0) A.lse[tok * A.H_q + hq] = (m + log2f(l)) * 0.693147180559945309f;
+}
+
+// A warp joins the parts of one (token, query head).
+template <typename T, int D>
+__global__ void __launch_bounds__(128) attend_join_kernel(const AttendArgs A, int ns) {
+  const int64_t row = blockIdx.x * static_cast<int64_t>(4) + (threadIdx.x >> 5);
+  const int64_t n = static_cast<int64_t>(A.n_tok) * A.H_q;
+  if (row >= n) return;
+  const int lane = threadIdx.x & 31;
+  float m = -INFINITY;
+  for (int p = 0; p < ns; ++p) m = fmaxf(m, A.part_ml[p * n + row].x);
+  const float base = m == -INFINITY ? 0.f : m;
+  float acc[D / 32], l = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) acc[i] = 0.f;
+  for (int p = 0; p < ns; ++p) {
+    const float2 ml = A.part_ml[p * n + row];
+    if (ml.x == -INFINITY && ml.y == 0.f) continue;  // a part that saw nothing
+    const float w = exp2f(ml.x - base);
+    l = fmaf(ml.y, w, l);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) acc[i] = fmaf(A.part_o[(p * n + row) * D + lane + 32 * i], w, acc[i]);
+  }
+  const int64_t tok = row / A.H_q;
+  const int hq = static_cast<int>(row - tok * A.H_q);
+  T* dst = reinterpret_cast<T*>(A.out) + tok * A.o_row + hq * A.o_head;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) dst[lane + 32 * i] = from_float<T>(acc[i] * inv);
+  if (A.lse && lane == 0) A.lse[row] = (m + log2f(l)) * 0.693147180559945309f;
+}
+
+template <typename T, int KIND, int D>
+hf_status launch_general(const CacheArgs& c, const AttendArgs& a, int max_kv, cudaStream_t stream) {
+  const int64_t tiles = most_tiles(a.n_tok, a.G, c.n_seq, kRows);
+  // keys are split where the tiles alone leave SMs idle, in parts of 128 keys at
+  // least, as far as the workspace goes
+  int64_t ns = std::min<int64_t>(2 * device_sm_count() / std::max<int64_t>(tiles * c.H, 1), (max_kv + 127) / 128);
+  ns = std::min<int64_t>(ns, part_rows(device_sm_count()) / (static_cast<int64_t>(a.n_tok) * a.H_q));
+  ns = std::max<int64_t>(1, std::min<int64_t>(ns, 64));
+  auto kern = attend_general_kernel<T, KIND, D>;
+  HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                   static_cast<int>(general_smem<D>())),
+              "hf_attend: shared memory size");
+  kern<<<dim3(static_cast<unsigned>(tiles), c.H, static_cast<unsigned>(ns)), kThreads, general_smem<D>(), stream>>>(
+      c, a, static_cast<int>(ns));
+  HF_CUDA_TRY(cudaGetLastError(), "hf_attend: launch");
+  if (ns > 1) return launch_join(sizeof(T) == 2 ? HF_BF16 : HF_F32, D, a, static_cast<int>(ns), stream);
+  return HF_OK;
+}
+
+template <int D>
+hf_status launch_join_d(hf_dtype dtype, const AttendArgs& a, int ns, cudaStream_t stream) {
+  const unsigned blocks = static_cast<unsigned>((static_cast<int64_t>(a.n_tok) * a.H_q + 3) / 4);
+  if (dtype == HF_BF16)
+    attend_join_kernel<__nv_bfloat16, D><<<blocks, 128, 0, stream>>>(a, ns);
+  else
+    attend_join_kernel<float, D><<<blocks, 128, 0, stream>>>(a, ns);
+  HF_CUDA_TRY(cudaGetLastError(), "hf_attend: joining launch");
+  return HF_OK;
+}
+
+template <int D>
+hf_status attend_general(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, hf_dtype dtype, int max_kv,
+                         cudaStream_t stream) {
+  if constexpr (D % 64 == 0) {
+    if (kind == HF_CACHE_Q4)
+      return dtype == HF_BF16 ? launch_general<__nv_bfloat16, HF_CACHE_Q4, D>(c, a, max_kv, stream)
+                              : launch_general<float, HF_CACHE_Q4, D>(c, a, max_kv, stream);
+  }
+  return dtype == HF_BF16 ? launch_general<__nv_bfloat16, HF_CACHE_BF16, D>(c, a, max_kv, stream)
+                          : launch_general<float, HF_CACHE_F32, D>(c, a, max_kv, stream);
+}
+
+size_t workspace_bytes_for(int D) {
+  return HF_ATTEND_ZEROED + static_cast<size_t>(part_rows(device_sm_count())) * (D + 2) * sizeof(float);
+}
+
+}  // namespace
+
+hf_status launch_join(hf_dtype dtype, int D, const AttendArgs& a, int ns, cudaStream_t stream) {
+  switch (D) {
+    case 32: return launch_join_d<32>(dtype, a, ns, stream);
+    case 64: return launch_join_d<64>(dtype, a, ns, stream);
+    case 96: return launch_join_d<96>(dtype, a, ns, stream);
+    case 128: return launch_join_d<128>(dtype, a, ns, stream);
+    default: return launch_join_d<256>(dtype, a, ns, stream);
+  }
+}
+
+}  // namespace hf
+
+using namespace hf;
+
+extern "C" hf_status hf_attend_workspace_size(const hf_cache* cache, size_t* bytes) {
+  CacheArgs c;
+  const hf_status st = cache_args("hf_attend_workspace_size", cache, &c);
+  if (st != HF_OK) return st;
+  if (!bytes) return bad_argument("hf_attend_workspace_size", "null output");
+  *bytes = workspace_bytes_for(c.D);
+  return HF_OK;
+}
+
+extern "C" hf_status hf_attend(const hf_cache* cache, const hf_attend_desc* d, void* d_workspace,
+                               size_t workspace_bytes, hf_stream_t stream_) {
+  const char* who = "hf_attend";
+  CacheArgs c;
+  const hf_status st = cache_args(who, cache, &c);
+  if (st != HF_OK) return st;
+  if (!d) return bad_argument(who, "null descriptor");
+  if (d->dtype != HF_BF16 && d->dtype != HF_F32) return bad_argument(who, "unknown dtype");
+  if (cache->kind != HF_CACHE_Q4 && (cache->kind == HF_CACHE_F32) != (d->dtype == HF_F32))
+    return bad_argument(who, "dtype must be the cache's");
+  if (d->H_q < 1 || d->H_q % c.H || d->H_q / c.H > 256) return bad_argument(who, "H_q must be a multiple of H, at most 256 H");
+  if (d->n_tok < 0 || d->max_q_len < 0 || d->max_kv_len < 0) return bad_argument(who, "sizes must not be negative");
+  if (static_cast<int64_t>(d->n_tok) * d->H_q > (1ll << 30)) return bad_argument(who, "n_tok * H_q must not pass 2^30");
+  if (d->causal != 0 && d->causal != 1) return bad_argument(who, "causal is a flag: 0 or 1");
+  if (!std::isfinite(d->scale) || d->scale < 0.f) return bad_argument(who, "scale must be finite and not negative");
+  if (d->n_tok > 0 && (!d->d_q_ptr || !d->d_kv_len || !d->d_q || !d->d_out)) return bad_argument(who, "null pointer");
+  if ((reinterpret_cast<uintptr_t>(d->d_q) | reinterpret_cast<uintptr_t>(d->d_out)) & 15u)
+    return bad_argument(who, "queries and outputs must be 16-byte aligned");
+  AttendArgs a = {};
+  const int es = d->dtype == HF_F32 ? 4 : 2;
+  a.q_row = d->q_row_stride, a.q_head = d->q_head_stride;
+  a.o_row = d->out_row_stride, a.o_head = d->out_head_stride;
+  if (!fill_strides(&a.q_row, &a.q_head, d->H_q, c.D, es) || !fill_strides(&a.o_row, &a.o_head, d->H_q, c.D, es))
+    return bad_argument(who, "strides must be positive multiples of 16 bytes");
+  if (!d_workspace || reinterpret_cast<uintptr_t>(d_workspace) & 255u || workspace_bytes < workspace_bytes_for(c.D)) {
+    set_error("hf_attend: the workspace must be 256-byte aligned and of hf_attend_workspace_size bytes");
+    return HF_ERR_WORKSPACE;
+  }
+  if (d->n_tok == 0) return HF_OK;
+  a.q = static_cast<const char*>(d->d_q);
+  a.out = static_cast<char*>(d->d_out);
+  a.lse = d->d_lse;
+  a.q_ptr = d->d_q_ptr;
+  a.kv_len = d->d_kv_len;
+  a.n_tok = d->n_tok;
+  a.H_q = d->H_q;
+  a.G = d->H_q / c.H;
+  a.causal = d->causal;
+  a.scale_log2 = (d->scale > 0.f ? d->scale : 1.f / std::sqrt(static_cast<float>(c.D))) * 1.44269504088896341f;
+  char* ws = static_cast<char*>(d_workspace);
+  a.zeroed = reinterpret_cast<int32_t*>(ws);
+  a.part_o = reinterpret_cast<float*>(ws + HF_ATTEND_ZEROED);
+  a.part_ml = reinterpret_cast<float2*>(a.part_o + part_rows(device_sm_count()) * c.D);
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
+  const int max_kv = static_cast<int>(std::min<int64_t>(d->max_kv_len, c.rows));
+  switch (c.D) {
+    case 32: return attend_general<32>(c, a, cache->kind, d->dtype, max_kv, stream);
+    case 64: return attend_general<64>(c, a, cache->kind, d->dtype, max_kv, stream);
+    case 96: return attend_general<96>(c, a, cache->kind, d->dtype, max_kv, stream);
+    case 128: return attend_general<128>(c, a, cache->kind, d->dtype, max_kv, stream);
+    default: return attend_general<256>(c, a, cache->kind, d->dtype, max_kv, stream);
+  }
+}

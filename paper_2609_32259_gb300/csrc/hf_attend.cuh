@@ -1,0 +1,105 @@
+// What the attention kernels share: arguments, the rows of a tile, partial results.
+//
+// Queries of one KV head are flattened to rows (token, head of the group): row
+// r of a sequence is token r / G and head r % G of the group's G.  A query of
+// token i sees the first `limit` cache rows, limit = kv_len - n + i + 1 (causal)
+// or kv_len.
+//
+// A softmax over keys that are split between blocks keeps, for each part, the
+// unnormalised output o, the maximum m of the scores (times log2 e) and the sum
+// l of 2^(score - m); parts join as o = sum o_p 2^(m_p - m) / sum l_p 2^(m_p - m).
+#pragma once
+
+#include "hf_cache.cuh"
+
+namespace hf {
+
+struct AttendArgs {
+  const char* q;
+  char* out;
+  float* lse;
+  const int32_t* q_ptr;
+  const int32_t* kv_len;
+  int64_t q_row, q_head, o_row, o_head;
+  int32_t n_tok, H_q, G;
+  int32_t causal;
+  float scale_log2;  // scale * log2(e)
+  float* part_o;     // partial outputs [part rows][D]
+  float2* part_ml;   // their m and l
+  int32_t* zeroed;   // counters, zero between calls
+};
+
+// Rows of partial results that a workspace holds.
+inline int64_t part_rows(int sm_count) { return 2 * 256 * static_cast<int64_t>(sm_count); }
+
+// A sequence's tokens and cache rows, made safe: tokens inside the packed
+// arrays, rows inside the cache.
+struct SeqSpan {
+  int first, n, kv;
+};
+__device__ __forceinline__ SeqSpan seq_span(const CacheArgs& C, const AttendArgs& A, int s) {
+  SeqSpan r;
+  const int a = A.q_ptr[s], b = A.q_ptr[s + 1];
+  r.first = min(max(a, 0), A.n_tok);
+  r.n = max(min(b, A.n_tok) - r.first, 0);
+  if (r.first != a || (b != r.first + r.n)) set_status(C, HF_CHECK_BAD_OFFSETS);
+  const int64_t kv = A.kv_len[s], cap = cache_capacity(C, s);
+  r.kv = static_cast<int>(kv < 0 ? 0 : kv > cap ? (cap < 0 ? 0 : cap) : kv);
+  if (kv != r.kv) set_status(C, HF_CHECK_CAPACITY);
+  return r;
+}
+
+// Cache rows that row r's query sees.
+__device__ __forceinline__ int seen(const SeqSpan& s, int causal, int token) {
+  return causal ? min(max(s.kv - s.n + token + 1, 0), s.kv) : s.kv;
+}
+
+// The sequence of tile `tile` (tiles of `rows` flattened rows, sequence by
+// sequence) and the tile's number in it, found by a whole warp; seq = n_seq
+// where there is no such tile.
+struct TilePlace {
+  int seq, at, tiles;
+};
+__device__ __forceinline__ TilePlace find_tile(const CacheArgs& C, const AttendArgs& A, int rows, int tile) {
+  const int lane = threadIdx.x & 31;
+  int before = 0;
+  for (int base = 0; base < C.n_seq; base += 32) {
+    const int i = base + lane;
+    int n = 0;
+    if (i < C.n_seq) {
+      const int a = min(max(A.q_ptr[i], 0), A.n_tok), b = min(A.q_ptr[i + 1], A.n_tok);
+      if (b > a) n = static_cast<int>((static_cast<int64_t>(b - a) * A.G + rows - 1) / rows);
+    }
+    int sum = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += v;
+    }
+    const unsigned past = __ballot_sync(0xffffffffu, before + sum > tile);
+    if (past) {
+      const int l = __ffs(past) - 1;
+      const int upto = __shfl_sync(0xffffffffu, sum, l), mine = __shfl_sync(0xffffffffu, n, l);
+      return {base + l, tile - (before + upto - mine), mine};
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  return {C.n_seq, 0, 0};
+}
+
+// Tiles of `rows` flattened rows at most, over all sequences.
+inline int64_t most_tiles(int64_t n_tok, int G, int n_seq, int rows) {
+  return n_tok * G / rows + (n_seq < n_tok ? n_seq : n_tok);
+}
+
+template <typename T>
+__device__ __forceinline__ T from_float(float v);
+template <>
+__device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// Joins `ns` parts of every (token, query head), [part][token][head].
+hf_status launch_join(hf_dtype dtype, int D, const AttendArgs& a, int ns, cudaStream_t stream);
+
+}  // namespace hf

@@ -1,0 +1,524 @@
+// Appending keys and values to a receiver's cache, and reading them back: the
+// path of every token that the receiver adds behind a transferred context.
+//
+// Append, token i of sequence s at cache row t = start + i and position p:
+//   x' = x g / sqrt(mean(x^2) + eps)                       (where a norm is given)
+//   y_d = x'_d cos - x'_{d+D/2} sin,  y_{d+D/2} = x'_{d+D/2} cos + x'_d sin
+// for keys and queries, values as they are, rounded once to what the cache
+// holds.  A 4-bit group of 32 channels takes scale = max|y| / 7 to 5 significant
+// bits and codes rint(y / scale) + 8.
+//
+// Bound by HBM: every key, value and query is read once and written once.  A
+// warp takes one token (its sequence, row and position are found once), 4 lanes
+// a head (2 where D / 16 is not a multiple of 4), each lane the 8-channel
+// chunks m, m + 4, ... of it: chunk c and its rotation partner c + D / 16 fall to
+// one lane, a 4-bit group is one chunk of each of the 4 lanes, and the codes of
+// a lane are D / 8 contiguous bytes of the row.
+#include <algorithm>
+#include <cmath>
+#include <string>
+
+#include "hf_cache.cuh"
+
+namespace hf {
+
+hf_status bad_argument(const char* who, const char* what) {
+  set_error(std::string(who) + ": " + what);
+  return HF_ERR_INVALID_ARGUMENT;
+}
+
+hf_status cache_args(const char* who, const hf_cache* c, CacheArgs* a) {
+  if (!c) return bad_argument(who, "null cache");
+  if (c->kind != HF_CACHE_BF16 && c->kind != HF_CACHE_F32 && c->kind != HF_CACHE_Q4)
+    return bad_argument(who, "unknown cache kind");
+  if (c->H < 1 || c->H > 1024 || c->D < 1) return bad_argument(who, "H in [1, 1024] and D >= 1");
+  const bool q4 = c->kind == HF_CACHE_Q4;
+  if (c->D != 64 && c->D != 128 && c->D != 256 && (q4 || (c->D != 32 && c->D != 96))) {
+    set_error(std::string(who) + ": unsupported: head width 32, 64, 96, 128 or 256 (4-bit: 64, 128, 256)");
+    return HF_ERR_UNSUPPORTED;
+  }
+  if (c->n_seq < 1 || c->n_seq > kMaxReq) return bad_argument(who, "n_seq in [1, 1024]");
+  if (c->rows < 0 || c->rows > 0x7fffffffll) return bad_argument(who, "rows in [0, 2^31)");
+  if (c->rows > 0 && (!c->d_k || !c->d_v)) return bad_argument(who, "null keys or values");
+  if (q4 && c->rows > 0 && (!c->d_k_scale || !c->d_v_scale)) return bad_argument(who, "a 4-bit cache needs its scales");
+  if ((reinterpret_cast<uintptr_t>(c->d_k) | reinterpret_cast<uintptr_t>(c->d_v)) & 15u)
+    return bad_argument(who, "keys and values must be 16-byte aligned");
+  if (q4 && ((reinterpret_cast<uintptr_t>(c->d_k_scale) | reinterpret_cast<uintptr_t>(c->d_v_scale)) &
+             static_cast<uintptr_t>(c->D / 16 - 1)))
+    return bad_argument(who, "scales must be aligned to a row's, D / 16 bytes");
+  *a = CacheArgs{};
+  a->row_stride = c->row_stride;
+  a->head_stride = c->head_stride;
+  if (q4 && (c->row_stride || c->head_stride)) return bad_argument(who, "a 4-bit cache takes no strides");
+  if (!fill_strides(&a->row_stride, &a->head_stride, c->H, c->D, c->kind == HF_CACHE_F32 ? 4 : 2))
+    return bad_argument(who, "cache strides must be positive multiples of 16 bytes");
+  if (c->d_block_table) {
+    if (c->block_size < 1 || c->max_blocks_per_seq < 1 || c->rows % c->block_size)
+      return bad_argument(who, "a paged cache needs block_size >= 1 dividing rows and max_blocks_per_seq >= 1");
+  } else if (!c->d_row0 && c->n_seq > 1) {
+    return bad_argument(who, "a contiguous cache of several sequences needs d_row0");
+  }
+  a->k = static_cast<char*>(c->d_k);
+  a->v = static_cast<char*>(c->d_v);
+  a->ks = static_cast<char*>(c->d_k_scale);
+  a->vs = static_cast<char*>(c->d_v_scale);
+  a->table = c->d_block_table;
+  a->row0 = c->d_block_table ? nullptr : c->d_row0;
+  a->status = c->d_status;
+  a->rows = c->rows;
+  a->H = c->H;
+  a->D = c->D;
+  a->n_seq = c->n_seq;
+  a->block_size = c->d_block_table ? c->block_size : 1;
+  a->block_shift = -1;
+  if ((a->block_size & (a->block_size - 1)) == 0)
+    for (a->block_shift = 0; (1 << a->block_shift) < a->block_size;) ++a->block_shift;
+  a->max_blocks = c->max_blocks_per_seq;
+  return HF_OK;
+}
+
+namespace {
+
+constexpr int kWarps = 4;  // tokens a block
+
+struct TokenArgs {
+  const int32_t* tok_ptr;
+  const int32_t* start;
+  int32_t n_tok;
+};
+struct AppendArgs {
+  TokenArgs t;
+  const char* k;
+  const char* v;
+  const char* q;
+  char* q_out;
+  int64_t k_row, k_head, v_row, v_head, q_row, q_head;
+  const float* rope;
+  const int32_t* pos0;
+  const float* k_norm;
+  const float* q_norm;
+  int32_t rope_len, H_q;
+  float eps;
+};
+struct ReadArgs {
+  TokenArgs t;
+  char* k;
+  char* v;
+  int64_t k_row, k_head, v_row, v_head;
+};
+
+// How the lanes of a warp lie on heads of D channels.
+template <int D>
+struct Lanes {
+  static constexpr int kPerHead = D % 64 == 0 ? 4 : 2;
+  static constexpr int kHeads = 32 / kPerHead;         // heads a warp takes at once
+  static constexpr int kChunks = D / 8 / kPerHead;     // 8-channel chunks a lane
+};
+
+// Eight channels.
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float* x) {
+  const uint4 u = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load8(const float* p, float* x) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x) {
+  *reinterpret_cast<uint4*>(p) = pack16(x, static_cast<const __nv_bfloat16*>(nullptr));
+}
+__device__ __forceinline__ void store8(float* p, const float* x) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+// N 32-bit words at p, N * 4 bytes aligned to at most 16.
+template <int N>
+__device__ __forceinline__ void store_words(void* p, const uint32_t* w) {
+  if constexpr (N == 1) {
+    *static_cast<uint32_t*>(p) = w[0];
+  } else if constexpr (N == 2) {
+    *static_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+      static_cast<uint4*>(p)[i / 4] = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+  }
+}
+template <int N>
+__device__ __forceinline__ void load_words(const void* p, uint32_t* w) {
+  if constexpr (N == 1) {
+    w[0] = *static_cast<const uint32_t*>(p);
+  } else if constexpr (N == 2) {
+    const uint2 u = *static_cast<const uint2*>(p);
+    w[0] = u.x, w[1] = u.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const uint4 u = static_cast<const uint4*>(p)[i / 4];
+      w[i] = u.x, w[i + 1] = u.y, w[i + 2] = u.z, w[i + 3] = u.w;
+    }
+  }
+}
+
+// A head's channels x (this lane's chunks) as 4-bit codes and scales; called by
+// whole warps, for heads that are stored or not.
+template <int D>
+__device__ __forceinline__ void store_q4(char* codes, char* scales, int m, bool store, const float (&x)[D / 32][8]) {
+  constexpr int NG = D / 32;  // groups, one chunk of each a lane
+  uint32_t half[2 * NG], sc[NG];
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    float a = fabsf(x[g][0]);
+    bool nan = a != a;
+#pragma unroll
+    for (int e = 1; e < 8; ++e) {
+      a = fmaxf(a, fabsf(x[g][e]));
+      nan |= x[g][e] != x[g][e];
+    }
+    if (nan) a = __int_as_float(0x7f800000);
+    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
+    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
+    const float s = q4_scale(a);
+    sc[g] = __float_as_uint(s) >> 16;
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      // zero and NaN scales: every code is 8
+      const float c = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(x[g][e], s)), -7.f), 7.f) : 0.f;
+      w |= static_cast<uint32_t>(static_cast<int>(c) + 8) << (4 * e);
+    }
+    half[g] = w & 0xffffu;       // channels 4 j .. + 3 of the group, j = 2 m
+    half[NG + g] = w >> 16;      // j = 2 m + 1
+  }
+  if (!store) return;
+  uint32_t w[NG];
+#pragma unroll
+  for (int i = 0; i < NG; ++i) w[i] = half[2 * i] | half[2 * i + 1] << 16;
+  store_words<NG>(codes + m * (D / 8), w);
+  if (m == 0) {
+    uint32_t s2[NG / 2];
+#pragma unroll
+    for (int i = 0; i < NG / 2; ++i) s2[i] = sc[2 * i] | sc[2 * i + 1] << 16;
+    store_words<NG / 2>(scales, s2);
+  }
+}
+
+template <typename T, int KIND, int D>
+__global__ void __launch_bounds__(32 * kWarps) append_kernel(const CacheArgs C, const AppendArgs A) {
+  using L = Lanes<D>;
+  constexpr int NC = L::kChunks;
+  const int lane = threadIdx.x & 31;
+  const int tok = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  if (tok >= A.t.n_tok) return;
+  const int seq = sequence_of(A.t.tok_ptr, C.n_seq, tok);
+  const int first = seq < C.n_seq ? A.t.tok_ptr[seq] : 0;
+  if (seq >= C.n_seq || first > tok || first < 0) {
+    if (lane == 0) set_status(C, HF_CHECK_BAD_OFFSETS);
+    return;
+  }
+  const int64_t t = static_cast<int64_t>(A.t.start[seq]) + (tok - first);
+  const int64_t pos = t + (A.pos0 ? A.pos0[seq] : 0);
+  if (t < 0 || (A.rope && (pos < 0 || pos >= A.rope_len))) {
+    if (lane == 0) set_status(C, HF_CHECK_CAPACITY);
+    return;
+  }
+  const int row = cache_row(C, seq, t);
+  if (row < 0) return;
+  const float* rope = A.rope ? A.rope + pos * D : nullptr;
+
+  const int m = lane % L::kPerHead;
+  const int n_heads = 2 * C.H + A.H_q;
+  for (int h0 = blockIdx.y * L::kHeads; h0 < n_heads; h0 += gridDim.y * L::kHeads) {
+    const int hh = h0 + lane / L::kPerHead;
+    const bool live = hh < n_heads;
+    const int role = hh < C.H ? 0 : hh < 2 * C.H ? 1 : 2;  // key, value, query
+    const int h = role == 0 ? hh : role == 1 ? hh - C.H : hh - 2 * C.H;
+    float x[NC][8];
+    const T* src = role == 0   ? reinterpret_cast<const T*>(A.k) + tok * A.k_row + h * A.k_head
+                   : role == 1 ? reinterpret_cast<const T*>(A.v) + tok * A.v_row + h * A.v_head
+                               : reinterpret_cast<const T*>(A.q) + tok * A.q_row + h * A.q_head;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      if (live) {
+        load8(src + 8 * (m + L::kPerHead * i), x[i]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
+      }
+    }
+    const float* g = role == 0 ? A.k_norm : role == 2 ? A.q_norm : nullptr;
+    if (A.k_norm || A.q_norm) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = fmaf(x[i][e], x[i][e], sum);
+#pragma unroll
+      for (int o = 1; o < L::kPerHead; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if (g) {
+        const float r = 1.f / sqrtf(sum / D + A.eps);
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+          float w[8];
+          load8(g + 8 * (m + L::kPerHead * i), w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[i][e] = x[i][e] * r * w[e];
+        }
+      }
+    }
+    if (rope && role != 1) {
+#pragma unroll
+      for (int i = 0; i < NC / 2; ++i) {
+        float cs[16];
+        load8(rope + 16 * (m + L::kPerHead * i), cs);
+        load8(rope + 16 * (m + L::kPerHead * i) + 8, cs + 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          // rounded one by one: 4-bit codes must not hang on what is contracted
+          const float a = x[i][e], b = x[i + NC / 2][e], c = cs[2 * e], s = cs[2 * e + 1];
+          x[i][e] = __fsub_rn(__fmul_rn(a, c), __fmul_rn(b, s));
+          x[i + NC / 2][e] = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
+        }
+      }
+    }
+    if constexpr (KIND == HF_CACHE_Q4) {
+      if (h0 < 2 * C.H) {  // all lanes join the groups' maxima
+        const int64_t at = static_cast<int64_t>(role < 2 ? h : 0) * C.rows + row;
+        store_q4<D>((role == 1 ? C.v : C.k) + at * (D / 2), (role == 1 ? C.vs : C.ks) + at * (D / 16), m,
+                    live && role < 2, x);
+      }
+    } else {
+      if (live && role < 2) {
+        T* dst = reinterpret_cast<T*>(role == 1 ? C.v : C.k) + row * C.row_stride + h * C.head_stride;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) store8(dst + 8 * (m + L::kPerHead * i), x[i]);
+      }
+    }
+    if (live && role == 2) {
+      T* dst = reinterpret_cast<T*>(A.q_out) + tok * A.q_row + h * A.q_head;
+#pragma unroll
+      for (int i = 0; i < NC; ++i) store8(dst + 8 * (m + L::kPerHead * i), x[i]);
+    }
+  }
+}
+
+template <typename T, int KIND, int D>
+__global__ void __launch_bounds__(32 * kWarps) read_kernel(const CacheArgs C, const ReadArgs A) {
+  using L = Lanes<D>;
+  constexpr int NC = L::kChunks;
+  const int lane = threadIdx.x & 31;
+  const int tok = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  if (tok >= A.t.n_tok) return;
+  const int seq = sequence_of(A.t.tok_ptr, C.n_seq, tok);
+  const int first = seq < C.n_seq ? A.t.tok_ptr[seq] : 0;
+  if (seq >= C.n_seq || first > tok || first < 0) {
+    if (lane == 0) set_status(C, HF_CHECK_BAD_OFFSETS);
+    return;
+  }
+  const int64_t t = static_cast<int64_t>(A.t.start[seq]) + (tok - first);
+  if (t < 0 && lane == 0) set_status(C, HF_CHECK_CAPACITY);
+  const int row = t < 0 ? -1 : cache_row(C, seq, t);
+  const int m = lane % L::kPerHead;
+  for (int h0 = blockIdx.y * L::kHeads; h0 < 2 * C.H; h0 += gridDim.y * L::kHeads) {
+    const int hh = h0 + lane / L::kPerHead;
+    if (hh >= 2 * C.H) break;
+    const bool val = hh >= C.H;
+    const int h = val ? hh - C.H : hh;
+    float x[NC][8];
+    if (row < 0) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
+    } else if constexpr (KIND == HF_CACHE_Q4) {
+      constexpr int NG = D / 32;
+      const int64_t at = static_cast<int64_t>(h) * C.rows + row;
+      uint32_t w[NG], s2[NG / 2];
+      load_words<NG>((val ? C.v : C.k) + at * (D / 2) + m * (D / 8), w);
+      load_words<NG / 2>((val ? C.vs : C.ks) + at * (D / 16), s2);
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        const float s = __uint_as_float(g & 1 ? s2[g / 2] & 0xffff0000u : s2[g / 2] << 16);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int i = j * NG + g;  // halfword
+          const uint32_t half = w[i / 2] >> (16 * (i & 1));
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            x[g][4 * j + e] = s * static_cast<float>(static_cast<int>((half >> (4 * e)) & 15u) - 8);
+        }
+      }
+    } else {
+      const T* src = reinterpret_cast<const T*>(val ? C.v : C.k) + row * C.row_stride + h * C.head_stride;
+#pragma unroll
+      for (int i = 0; i < NC; ++i) load8(src + 8 * (m + L::kPerHead * i), x[i]);
+    }
+    T* dst = val ? reinterpret_cast<T*>(A.v) + tok * A.v_row + h * A.v_head
+                 : reinterpret_cast<T*>(A.k) + tok * A.k_row + h * A.k_head;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) store8(dst + 8 * (m + L::kPerHead * i), x[i]);
+  }
+}
+
+struct InvFreq {
+  float f[kMaxHeadDim / 2];
+};
+
+__global__ void rope_table_kernel(const InvFreq inv, int half, int pos0, int64_t n, float2* out) {
+  const int64_t i = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x;
+  if (i >= n) return;
+  float s, c;
+  rope_sincos(pos0 + static_cast<int>(i / half), inv.f[i % half], &s, &c);
+  out[i] = make_float2(c, s);
+}
+
+// Warps of a token where there are few tokens: its heads' steps are shared out
+// until every SM has some 16 warps.
+template <int D>
+dim3 token_grid(int n_tok, int heads) {
+  const int blocks = (n_tok + kWarps - 1) / kWarps;
+  const int steps = (heads + Lanes<D>::kHeads - 1) / Lanes<D>::kHeads;
+  const int want = (device_sm_count() * 16 / kWarps + blocks - 1) / blocks;
+  return dim3(blocks, std::max(1, std::min(steps, want)));
+}
+
+template <typename T, int KIND, int D>
+hf_status launch_append(const CacheArgs& c, const AppendArgs& a, cudaStream_t stream) {
+  append_kernel<T, KIND, D><<<token_grid<D>(a.t.n_tok, 2 * c.H + a.H_q), 32 * kWarps, 0, stream>>>(c, a);
+  HF_CUDA_TRY(cudaGetLastError(), "hf_cache_append: launch");
+  return HF_OK;
+}
+template <typename T, int KIND, int D>
+hf_status launch_read(const CacheArgs& c, const ReadArgs& a, cudaStream_t stream) {
+  read_kernel<T, KIND, D><<<token_grid<D>(a.t.n_tok, 2 * c.H), 32 * kWarps, 0, stream>>>(c, a);
+  HF_CUDA_TRY(cudaGetLastError(), "hf_cache_read: launch");
+  return HF_OK;
+}
+
+// f of the kernel's element type, cache kind and head width.
+#define HF_CACHE_DISPATCH(f, dtype, kind, c, a, stream)                                             \
+  switch (c.D) {                                                                                    \
+    case 32: return dtype == HF_BF16 ? f<__nv_bfloat16, HF_CACHE_BF16, 32>(c, a, stream)            \
+                                     : f<float, HF_CACHE_F32, 32>(c, a, stream);                    \
+    case 96: return dtype == HF_BF16 ? f<__nv_bfloat16, HF_CACHE_BF16, 96>(c, a, stream)            \
+                                     : f<float, HF_CACHE_F32, 96>(c, a, stream);                    \
+    HF_CACHE_DISPATCH_Q4(f, 64, dtype, kind, c, a, stream)                                          \
+    HF_CACHE_DISPATCH_Q4(f, 128, dtype, kind, c, a, stream)                                         \
+    HF_CACHE_DISPATCH_Q4(f, 256, dtype, kind, c, a, stream)                                         \
+    default: return HF_ERR_UNSUPPORTED;                                                             \
+  }
+#define HF_CACHE_DISPATCH_Q4(f, D, dtype, kind, c, a, stream)                                       \
+  case D:                                                                                           \
+    if (kind == HF_CACHE_Q4)                                                                        \
+      return dtype == HF_BF16 ? f<__nv_bfloat16, HF_CACHE_Q4, D>(c, a, stream)                      \
+                              : f<float, HF_CACHE_Q4, D>(c, a, stream);                             \
+    return dtype == HF_BF16 ? f<__nv_bfloat16, HF_CACHE_BF16, D>(c, a, stream)                      \
+                            : f<float, HF_CACHE_F32, D>(c, a, stream);
+
+// What append and read ask of their token arrays.
+hf_status check_tokens(const char* who, const hf_cache* cache, hf_dtype dtype, int32_t n_tok,
+                       const void* tok_ptr, const void* start, const void* k, const void* v) {
+  if (dtype != HF_BF16 && dtype != HF_F32) return bad_argument(who, "unknown dtype");
+  if (cache->kind != HF_CACHE_Q4 && (cache->kind == HF_CACHE_F32) != (dtype == HF_F32))
+    return bad_argument(who, "dtype must be the cache's");
+  if (n_tok < 0) return bad_argument(who, "n_tok must not be negative");
+  if (n_tok > 0 && (!tok_ptr || !start || !k || !v)) return bad_argument(who, "null pointer");
+  if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15u)
+    return bad_argument(who, "keys and values must be 16-byte aligned");
+  return HF_OK;
+}
+
+}  // namespace
+}  // namespace hf
+
+using namespace hf;
+
+extern "C" hf_status hf_rope_table(int32_t D, double theta, const float* h_inv_freq, int32_t pos0,
+                                   int32_t n_pos, float* d_table, hf_stream_t stream_) {
+  const char* who = "hf_rope_table";
+  if (D < 2 || D > kMaxHeadDim || D % 2) return bad_argument(who, "D must be even, in [2, 256]");
+  if (!h_inv_freq && !(theta > 0.0)) return bad_argument(who, "needs theta > 0 or a table of inverse frequencies");
+  if (pos0 < 0 || n_pos < 0 || static_cast<int64_t>(pos0) + n_pos > (1 << 24))
+    return bad_argument(who, "positions must lie in [0, 2^24)");
+  if (n_pos > 0 && (!d_table || reinterpret_cast<uintptr_t>(d_table) & 15u))
+    return bad_argument(who, "the table must be 16-byte aligned device memory");
+  InvFreq inv = {};
+  for (int i = 0; i < D / 2; ++i) {
+    inv.f[i] = h_inv_freq ? h_inv_freq[i] : static_cast<float>(std::pow(theta, -2.0 * i / D));
+    if (!std::isfinite(inv.f[i])) return bad_argument(who, "inverse frequency not finite");
+  }
+  if (n_pos == 0) return HF_OK;
+  const int64_t n = static_cast<int64_t>(n_pos) * (D / 2);
+  rope_table_kernel<<<static_cast<unsigned>((n + 255) / 256), 256, 0, reinterpret_cast<cudaStream_t>(stream_)>>>(
+      inv, D / 2, pos0, n, reinterpret_cast<float2*>(d_table));
+  HF_CUDA_TRY(cudaGetLastError(), "hf_rope_table: launch");
+  return HF_OK;
+}
+
+extern "C" hf_status hf_cache_append(const hf_cache* cache, const hf_append_desc* d, hf_stream_t stream_) {
+  const char* who = "hf_cache_append";
+  CacheArgs c;
+  hf_status st = cache_args(who, cache, &c);
+  if (st != HF_OK) return st;
+  if (!d) return bad_argument(who, "null descriptor");
+  st = check_tokens(who, cache, d->dtype, d->n_tok, d->d_tok_ptr, d->d_start, d->d_k, d->d_v);
+  if (st != HF_OK) return st;
+  AppendArgs a = {};
+  const int es = d->dtype == HF_F32 ? 4 : 2;
+  a.k_row = d->k_row_stride, a.k_head = d->k_head_stride;
+  a.v_row = d->v_row_stride, a.v_head = d->v_head_stride;
+  a.q_row = d->q_row_stride, a.q_head = d->q_head_stride;
+  a.H_q = d->d_q ? d->H_q : 0;
+  if (d->d_q && (d->H_q < 1 || d->H_q > 65536 || !d->d_q_out)) return bad_argument(who, "queries need H_q >= 1 and d_q_out");
+  if (!fill_strides(&a.k_row, &a.k_head, c.H, c.D, es) || !fill_strides(&a.v_row, &a.v_head, c.H, c.D, es) ||
+      !fill_strides(&a.q_row, &a.q_head, std::max(a.H_q, 1), c.D, es))
+    return bad_argument(who, "strides must be positive multiples of 16 bytes");
+  if ((reinterpret_cast<uintptr_t>(d->d_q) | reinterpret_cast<uintptr_t>(d->d_q_out) |
+       reinterpret_cast<uintptr_t>(d->d_rope) | reinterpret_cast<uintptr_t>(d->d_k_norm) |
+       reinterpret_cast<uintptr_t>(d->d_q_norm)) & 15u)
+    return bad_argument(who, "queries, rotation table and norm weights must be 16-byte aligned");
+  if (d->d_rope && d->rope_len < 1) return bad_argument(who, "rope_len must be positive");
+  if ((d->d_k_norm || d->d_q_norm) && !(d->eps >= 0.f)) return bad_argument(who, "eps must not be negative");
+  if (d->n_tok == 0) return HF_OK;
+  a.t = {d->d_tok_ptr, d->d_start, d->n_tok};
+  a.k = static_cast<const char*>(d->d_k);
+  a.v = static_cast<const char*>(d->d_v);
+  a.q = static_cast<const char*>(d->d_q);
+  a.q_out = static_cast<char*>(d->d_q_out);
+  a.rope = d->d_rope;
+  a.rope_len = d->rope_len;
+  a.pos0 = d->d_pos0;
+  a.k_norm = d->d_k_norm;
+  a.q_norm = d->d_q_norm;
+  a.eps = d->eps;
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
+  HF_CACHE_DISPATCH(launch_append, d->dtype, cache->kind, c, a, stream)
+}
+
+extern "C" hf_status hf_cache_read(const hf_cache* cache, const hf_read_desc* d, hf_stream_t stream_) {
+  const char* who = "hf_cache_read";
+  CacheArgs c;
+  hf_status st = cache_args(who, cache, &c);
+  if (st != HF_OK) return st;
+  if (!d) return bad_argument(who, "null descriptor");
+  st = check_tokens(who, cache, d->dtype, d->n_tok, d->d_tok_ptr, d->d_start, d->d_k, d->d_v);
+  if (st != HF_OK) return st;
+  ReadArgs a = {};
+  const int es = d->dtype == HF_F32 ? 4 : 2;
+  a.k_row = d->k_row_stride, a.k_head = d->k_head_stride;
+  a.v_row = d->v_row_stride, a.v_head = d->v_head_stride;
+  if (!fill_strides(&a.k_row, &a.k_head, c.H, c.D, es) || !fill_strides(&a.v_row, &a.v_head, c.H, c.D, es))
+    return bad_argument(who, "strides must be positive multiples of 16 bytes");
+  if (d->n_tok == 0) return HF_OK;
+  a.t = {d->d_tok_ptr, d->d_start, d->n_tok};
+  a.k = static_cast<char*>(d->d_k);
+  a.v = static_cast<char*>(d->d_v);
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
+  HF_CACHE_DISPATCH(launch_read, d->dtype, cache->kind, c, a, stream)
+}

@@ -1,0 +1,108 @@
+// What the kernels that use a cache (append, read, attend) share: where a
+// sequence's rows are, and the 4-bit format.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <stdint.h>
+
+#include "hf_device.cuh"
+#include "hf_internal.h"
+
+namespace hf {
+
+constexpr int kQ4Group = 32;  // channels that share a scale
+
+// hf_cache as the kernels take it (strides filled in).
+struct CacheArgs {
+  char* k;
+  char* v;
+  char* ks;
+  char* vs;
+  const int32_t* table;
+  const int32_t* row0;
+  int32_t* status;
+  int64_t rows;
+  int64_t row_stride, head_stride;  // elements (bf16, fp32)
+  int32_t H, D, n_seq;
+  int32_t block_size, block_shift;  // shift >= 0: block_size is 2^shift
+  int32_t max_blocks;
+};
+
+// Checks a cache (`who`: the entry point, for messages) and fills `a`.
+hf_status cache_args(const char* who, const hf_cache* c, CacheArgs* a);
+// HF_ERR_INVALID_ARGUMENT with the message "<who>: <what>".
+hf_status bad_argument(const char* who, const char* what);
+
+// Row and head strides of a packed array as given or dense; false where they
+// are not positive multiples of 16 bytes.
+inline bool fill_strides(int64_t* row, int64_t* head, int heads, int D, int elem_bytes) {
+  if (*row == 0) *row = static_cast<int64_t>(heads) * D;
+  if (*head == 0) *head = D;
+  return *row > 0 && *head > 0 && (*row * elem_bytes) % 16 == 0 && (*head * elem_bytes) % 16 == 0;
+}
+
+__device__ __forceinline__ void set_status(const CacheArgs& c, int bit) {
+  if (c.status) atomicOr(c.status, bit);
+}
+
+// Rows that sequence s can have.
+__device__ __forceinline__ int64_t cache_capacity(const CacheArgs& c, int s) {
+  if (c.table) return static_cast<int64_t>(c.max_blocks) * c.block_size;
+  return c.rows - (c.row0 ? c.row0[s] : 0);
+}
+
+// Row of the buffers that holds row t >= 0 of sequence s, or -1 (and a status
+// bit) where there is none.
+__device__ __forceinline__ int cache_row(const CacheArgs& c, int s, int64_t t) {
+  if (c.table) {
+    int b, r;
+    if (c.block_shift >= 0) {
+      b = static_cast<int>(t >> c.block_shift);
+      r = static_cast<int>(t) & (c.block_size - 1);
+    } else {
+      b = static_cast<int>(t / c.block_size);
+      r = static_cast<int>(t - static_cast<int64_t>(b) * c.block_size);
+    }
+    if (b >= c.max_blocks) {
+      set_status(c, HF_CHECK_CAPACITY);
+      return -1;
+    }
+    const int64_t row = static_cast<int64_t>(c.table[static_cast<int64_t>(s) * c.max_blocks + b]) * c.block_size;
+    if (row < 0 || row + c.block_size > c.rows) {
+      set_status(c, HF_CHECK_BAD_BLOCK);
+      return -1;
+    }
+    return static_cast<int>(row) + r;
+  }
+  const int64_t row = (c.row0 ? c.row0[s] : 0) + t;
+  if (row < 0 || row >= c.rows) {
+    set_status(c, HF_CHECK_CAPACITY);
+    return -1;
+  }
+  return static_cast<int>(row);
+}
+
+// The sequence of packed token `tok`, found by a whole warp: the number of
+// sequences that end at or before it.  n_seq: there is none.
+__device__ __forceinline__ int sequence_of(const int32_t* tok_ptr, int n_seq, int tok) {
+  const int lane = threadIdx.x & 31;
+  int seq = 0;
+  for (int base = 0; base < n_seq; base += 32) {
+    const int i = base + lane;
+    const unsigned m = __ballot_sync(0xffffffffu, i < n_seq && tok_ptr[i + 1] <= tok);
+    seq += __popc(m);
+    if (m != 0xffffffffu) break;
+  }
+  return seq;
+}
+
+// scale of a 4-bit group with largest magnitude a: a / 7 to 5 significant bits,
+// half up (a carry goes into the exponent); 0 where it is below 2^-100, NaN
+// where a is not finite.
+__device__ __forceinline__ float q4_scale(float a) {
+  const float s = __uint_as_float((__float_as_uint(__fdiv_rn(a, 7.f)) + 0x40000u) & 0xFFF80000u);
+  if (!(a <= 3.0e38f)) return __int_as_float(0x7fc00000);
+  return s < 7.9e-31f ? 0.f : s;
+}
+
+}  // namespace hf

@@ -1,6 +1,7 @@
-"""One transfer direction end to end on one GPU: torch allocates the device
-buffers, the C ABI does the work (alignment CSR, plan metadata, the fused
-map).  No arithmetic of the method happens here.
+"""One transfer direction end to end on one GPU, and the receiver's use of the
+cache afterwards: torch allocates the device buffers, the C ABI does the work
+(alignment CSR, plan metadata, the fused map; appending to a cache, reading it,
+attention over it).  No arithmetic of the method happens here.
 """
 
 from __future__ import annotations
@@ -160,6 +161,225 @@ class TransferJob:
         if self.plan is not None:
             self.plan.destroy()
             self.plan = None
+
+
+def rope_table(n_pos: int, D: int, *, theta: float = 0.0, inv_freq=None, pos0: int = 0,
+               device="cuda", stream=None) -> torch.Tensor:
+    """cos and sin of positions pos0 .. pos0 + n_pos - 1, fp32 [n_pos, D/2, 2]
+    (what KVCache.append takes), with the transfer's angle arithmetic."""
+    t = torch.empty((n_pos, D // 2, 2), dtype=torch.float32, device=device)
+    B.rope_table(D, t, theta, inv_freq, pos0, _stream_of(t, stream))
+    return t
+
+
+def _stream_of(t: torch.Tensor, stream):
+    return torch.cuda.current_stream(t.device) if stream is None else stream
+
+
+def _rows(name, t, n, heads, D, dtype):
+    """Row and head stride of a [n, heads, D] tensor whose channels are dense."""
+    if t.shape != (n, heads, D) or t.dtype != dtype or (D > 1 and n * heads > 0 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be {dtype} [{n}, {heads}, {D}] with dense channels, got "
+                         f"{t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+    return t.stride(0), t.stride(1)
+
+
+def _ints(name, t, n):
+    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of {n} values")
+    return t.data_ptr()
+
+
+_TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
+_NAMES = {v: k for k, v in _TORCH.items()}
+
+
+class KVCache:
+    """The cache of a receiver: keys and values of n_seq sequences in `layers`
+    layers, as hf_transfer writes it or in 4 bits, and the calls that use it.
+
+    kind     "bf16", "f32" or "q4"
+    kv       bf16, f32: [layers, 2, rows, H * D] or [layers, 2, rows, H, D]
+             (a TransferJob's receiver, for instance); made here when None
+    codes, scales  q4: uint8 [layers, 2, H, rows, D/2], bf16 [layers, 2, H, rows, D/32]
+    block_table, block_size  paged: device int32 [n_seq, max_blocks]
+    row0     contiguous: device int32 [n_seq], the first row of each sequence
+             (None: 0, one sequence)
+    rows     rows to allocate when no buffers are given
+
+    Calls run on `stream` (None: torch's current stream) and return at once;
+    status() waits and returns the HF_CHECK_* bits that they left.  The workspace
+    of attend is the cache's: its attend calls belong on one stream, or in order.
+    """
+
+    def __init__(self, *, kind: str, H: int, D: int, n_seq: int, layers: int = 1,
+                 kv: Optional[torch.Tensor] = None, codes: Optional[torch.Tensor] = None,
+                 scales: Optional[torch.Tensor] = None, rows: Optional[int] = None,
+                 block_table: Optional[torch.Tensor] = None, block_size: int = 0,
+                 row0: Optional[torch.Tensor] = None, device="cuda"):
+        self.kind, self.H, self.D, self.n_seq = kind, int(H), int(D), int(n_seq)
+        B.CACHE_KINDS[kind]
+        if kind == "q4":
+            if codes is None:
+                codes = torch.full((layers, 2, H, rows, D // 2), 0x88, dtype=torch.uint8, device=device)
+                scales = torch.zeros((layers, 2, H, rows, D // 32), dtype=torch.bfloat16, device=device)
+            rows = codes.shape[3]
+            if (codes.dtype != torch.uint8 or codes.shape[1:] != (2, H, rows, D // 2)
+                    or scales is None or scales.dtype != torch.bfloat16
+                    or scales.shape != (codes.shape[0], 2, H, rows, D // 32)
+                    or not codes.is_contiguous() or not scales.is_contiguous()):
+                raise ValueError("codes must be uint8 [layers, 2, H, rows, D/2] and scales bf16 "
+                                 "[layers, 2, H, rows, D/32], contiguous")
+            self.codes, self.scales, self.kv = codes, scales, None
+            self.layers = codes.shape[0]
+            self.device = codes.device
+        else:
+            if kv is None:
+                kv = torch.zeros((layers, 2, rows, H, D), dtype=_TORCH[kind], device=device)
+            rows = kv.shape[2]
+            if (kv.dtype != _TORCH[kind] or kv.shape[1] != 2 or kv[0, 0].numel() != rows * H * D
+                    or not kv.is_contiguous()):
+                raise ValueError(f"kv must be {_TORCH[kind]} [layers, 2, rows, H * D], contiguous")
+            self.kv, self.codes, self.scales = kv, None, None
+            self.layers = kv.shape[0]
+            self.device = kv.device
+        self.rows = int(rows)
+        self.block_table, self.row0 = block_table, row0
+        self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._workspace: Optional[torch.Tensor] = None
+        max_blocks = 0
+        if block_table is not None:
+            max_blocks = block_table.shape[1]
+            _ints("block_table", block_table, n_seq * max_blocks)
+        elif row0 is not None:
+            _ints("row0", row0, n_seq)
+        self._descs = []
+        for l in range(self.layers):
+            d = B.CacheDesc(kind=B.CACHE_KINDS[kind], H=H, D=D, n_seq=n_seq, rows=self.rows,
+                            d_block_table=None if block_table is None else block_table.data_ptr(),
+                            block_size=int(block_size), max_blocks_per_seq=int(max_blocks),
+                            d_row0=None if row0 is None else row0.data_ptr(),
+                            d_status=self._status.data_ptr())
+            if kind == "q4":
+                d.d_k, d.d_v = codes[l, 0].data_ptr(), codes[l, 1].data_ptr()
+                d.d_k_scale, d.d_v_scale = scales[l, 0].data_ptr(), scales[l, 1].data_ptr()
+            else:
+                d.d_k, d.d_v = kv[l, 0].data_ptr(), kv[l, 1].data_ptr()
+            self._descs.append(d)
+
+    @classmethod
+    def of_tensors(cls, k: torch.Tensor, v: torch.Tensor, *, n_seq: int = 1,
+                   row0: Optional[torch.Tensor] = None) -> "KVCache":
+        """One layer's keys and values [rows, H, D] where they are (slices of a
+        larger tensor, with the same strides), for prompts that need no cache."""
+        self = cls.__new__(cls)
+        if k.dtype not in _NAMES or v.dtype != k.dtype or k.shape != v.shape or k.stride() != v.stride():
+            raise ValueError("k and v must have the same shape, strides and type (bf16 or f32)")
+        rows, H, D = k.shape
+        rs, hs = _rows("k", k, rows, H, D, k.dtype)
+        self.kind, self.H, self.D, self.n_seq, self.layers, self.rows = _NAMES[k.dtype], H, D, n_seq, 1, rows
+        self.kv, self.codes, self.scales, self.device = (k, v), None, None, k.device
+        self.block_table, self.row0 = None, row0
+        self._status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        self._workspace = None
+        if row0 is not None:
+            _ints("row0", row0, n_seq)
+        self._descs = [B.CacheDesc(kind=B.CACHE_KINDS[self.kind], H=H, D=D, n_seq=n_seq, rows=rows,
+                                   d_k=k.data_ptr(), d_v=v.data_ptr(), row_stride=rs, head_stride=hs,
+                                   d_row0=None if row0 is None else row0.data_ptr(),
+                                   d_status=self._status.data_ptr())]
+        return self
+
+    @classmethod
+    def of_job(cls, job: TransferJob) -> "KVCache":
+        """The receiver cache of a transfer, one sequence a request.  A contiguous
+        cache has no room behind a request's rows: append needs a paged one."""
+        n = len(job.r_tok_ptr) - 1
+        row0 = None
+        if job.paged is None:
+            row0 = torch.as_tensor(job.r_tok_ptr[:-1].copy()).to(job.device)
+        return cls(kind=job.dtype, H=job.H_r, D=job.D_r, n_seq=n, kv=job.receiver,
+                   block_table=job.block_table, block_size=job.paged.block_size if job.paged else 0,
+                   row0=row0)
+
+    def append(self, layer: int, k, v, tok_ptr, start, *, rope=None, q=None, q_out=None, k_norm=None,
+               q_norm=None, eps: float = 1e-6, pos0=None, stream=None) -> None:
+        """hf_cache_append: keys and values [n_tok, H, D] of packed new tokens
+        (sequence s: tok_ptr[s] .. tok_ptr[s+1], device int32) into rows
+        start[s] .. of the sequences; keys, and queries q [n_tok, H_q, D] into
+        q_out, normed (k_norm, q_norm fp32 [D]) and rotated (rope, see
+        rope_table) on the way."""
+        n, n_seq = k.shape[0], self.n_seq
+        dt = k.dtype
+        d = B.AppendDesc(dtype=B.DTYPES[_NAMES[dt]], n_tok=n, d_tok_ptr=_ints("tok_ptr", tok_ptr, n_seq + 1),
+                         d_start=_ints("start", start, n_seq), d_k=k.data_ptr(), d_v=v.data_ptr(), eps=eps)
+        d.k_row_stride, d.k_head_stride = _rows("k", k, n, self.H, self.D, dt)
+        d.v_row_stride, d.v_head_stride = _rows("v", v, n, self.H, self.D, dt)
+        if q is not None:
+            if q_out is None:
+                raise ValueError("q needs q_out")
+            d.H_q = q.shape[1]
+            d.d_q, d.d_q_out = q.data_ptr(), q_out.data_ptr()
+            d.q_row_stride, d.q_head_stride = _rows("q", q, n, d.H_q, self.D, dt)
+            if _rows("q_out", q_out, n, d.H_q, self.D, dt) != (d.q_row_stride, d.q_head_stride):
+                raise ValueError("q and q_out must have the same strides")
+        if rope is not None:
+            if rope.dtype != torch.float32 or rope.shape[1:] != (self.D // 2, 2) or not rope.is_contiguous():
+                raise ValueError("rope must be a contiguous fp32 tensor [n_pos, D/2, 2]")
+            d.d_rope, d.rope_len = rope.data_ptr(), rope.shape[0]
+        if pos0 is not None:
+            d.d_pos0 = _ints("pos0", pos0, n_seq)
+        for name, w in (("k_norm", k_norm), ("q_norm", q_norm)):
+            if w is not None:
+                if w.dtype != torch.float32 or w.numel() != self.D or not w.is_contiguous():
+                    raise ValueError(f"{name} must be a contiguous fp32 tensor of {self.D} values")
+                setattr(d, "d_" + name, w.data_ptr())
+        B.cache_append(self._descs[layer], d, _stream_of(k, stream))
+
+    def read(self, layer: int, k, v, tok_ptr, start, *, stream=None) -> None:
+        """hf_cache_read: rows start[s] .. of the sequences into packed k, v
+        [n_tok, H, D]."""
+        n = k.shape[0]
+        d = B.ReadDesc(dtype=B.DTYPES[_NAMES[k.dtype]], n_tok=n, d_tok_ptr=_ints("tok_ptr", tok_ptr, self.n_seq + 1),
+                       d_start=_ints("start", start, self.n_seq), d_k=k.data_ptr(), d_v=v.data_ptr())
+        d.k_row_stride, d.k_head_stride = _rows("k", k, n, self.H, self.D, k.dtype)
+        d.v_row_stride, d.v_head_stride = _rows("v", v, n, self.H, self.D, k.dtype)
+        B.cache_read(self._descs[layer], d, _stream_of(k, stream))
+
+    def attend(self, layer: int, q, out, q_ptr, kv_len, *, max_q_len: Optional[int] = None,
+               max_kv_len: Optional[int] = None, causal: bool = True, scale: float = 0.0, lse=None,
+               stream=None) -> None:
+        """hf_attend: out [n_tok, H_q, D] = attention of packed queries q (sequence
+        s: q_ptr[s] .. q_ptr[s+1]) over the first kv_len[s] rows of their
+        sequences; max_q_len and max_kv_len are upper bounds known on the host
+        (None: what the packed tokens and the cache allow); lse fp32 [n_tok, H_q]."""
+        n, H_q = q.shape[0], q.shape[1]
+        d = B.AttendDesc(dtype=B.DTYPES[_NAMES[q.dtype]], H_q=H_q, n_tok=n,
+                         d_q_ptr=_ints("q_ptr", q_ptr, self.n_seq + 1),
+                         d_kv_len=_ints("kv_len", kv_len, self.n_seq),
+                         max_q_len=n if max_q_len is None else max_q_len,
+                         max_kv_len=self.rows if max_kv_len is None else max_kv_len,
+                         causal=int(bool(causal)), scale=scale, d_q=q.data_ptr(), d_out=out.data_ptr())
+        d.q_row_stride, d.q_head_stride = _rows("q", q, n, H_q, self.D, q.dtype)
+        d.out_row_stride, d.out_head_stride = _rows("out", out, n, H_q, self.D, q.dtype)
+        if lse is not None:
+            if lse.dtype != torch.float32 or lse.shape != (n, H_q) or not lse.is_contiguous():
+                raise ValueError("lse must be a contiguous fp32 tensor [n_tok, H_q]")
+            d.d_lse = lse.data_ptr()
+        if self._workspace is None:
+            self._workspace = attend_workspace(self._descs[0], self.device)
+        B.attend(self._descs[layer], d, self._workspace, None, _stream_of(q, stream))
+
+    def status(self) -> int:
+        """HF_CHECK_* bits of the calls so far (waits for the device)."""
+        return int(self._status.item())
+
+
+def attend_workspace(desc: B.CacheDesc, device="cuda") -> torch.Tensor:
+    """A workspace for hf_attend (its counters zeroed)."""
+    ws = torch.empty(B.attend_workspace_size(desc), dtype=torch.uint8, device=device)
+    ws[:B.ATTEND_ZEROED].zero_()
+    return ws
 
 
 def job_from_workload(w, tok, sender, W, b, r, *, paged=None, knorm_w=None, r_pos0=None,
