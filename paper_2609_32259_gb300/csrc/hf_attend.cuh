@@ -99,6 +99,11 @@ __device__ __forceinline__ float from_float<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// The form for few query rows a KV head (hf_attend_rows.cu): bf16 queries, bf16
+// and 4-bit caches, D 64 and 128.  max_rows: tokens times G at most.
+bool attend_rows_takes(hf_cache_kind kind, hf_dtype dtype, int D);
+hf_status attend_rows(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_rows, cudaStream_t stream);
+
 // Joins `ns` parts of every (token, query head), [part][token][head].
 hf_status launch_join(hf_dtype dtype, int D, const AttendArgs& a, int ns, cudaStream_t stream);
 

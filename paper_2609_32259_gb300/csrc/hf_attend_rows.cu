@@ -1,0 +1,623 @@
+// Attention of few query rows over a long cache: a receiver's decoding steps.
+//
+// Bound by HBM: every cached key and value is read once, at 8 to 64 FLOP a byte.
+// So the work is cut by bytes and by nothing else: a unit is one (sequence, KV
+// head, chunk of 8 or 16 query rows), its keys are steps of 64 (4-bit: 128), and
+// the steps of all units, laid end to end, are shared out evenly over the blocks,
+// two or three of 4 warps on an SM.  A block whose share begins or ends inside a
+// unit leaves a partial result, and whoever is last at a unit joins them in
+// order (no sum depends on who that is).
+//
+// Each warp runs alone: 16 keys (4-bit: 32) at a time come by cp.async into a
+// ring of its own, two or three stages ahead, and the scores and outputs go
+// through the warp-level tensor instruction with the keys as rows:
+//   S^T [keys x queries] = K Q^T,   O^T [channels x queries] += V^T P^T,
+// so that eight queries fill its columns (M = 16 rows are keys or channels,
+// never padding), K comes as it lies and V transposed by ldmatrix, and P^T turns
+// from one layout to the other in two movmatrix.  A row's maximum moves only
+// when a score passes it by 2^8: until then sums stay below 2^8 of their
+// largest term, and most steps need one vote and no shuffle.
+//
+// 4-bit rows stay codes: the nibbles c of a word are masked in place and are, as
+// bf16 numbers, c 2^-133 and 16 c 2^-133 (subnormal, exact), one or two
+// operations for two codes.  Queries are scaled by 2^64 (and 2^60), and group
+// scales apply to the 32-channel partial scores in fp32; for the values they go
+// into P (one rounding, the one that P takes anyway).  The offset of 8 is the
+// score accumulator's start, -8 sum(q), and a further product with a constant
+// row for the values.
+#include <algorithm>
+
+#include "hf_attend.cuh"
+
+namespace hf {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr float kStretch = 8.f;  // log2 of what a score may pass the running maximum by
+
+__device__ __forceinline__ void cp_async_16_or_zero(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void cp_async_small(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(N), "r"(there ? N : 0)
+               : "memory");
+}
+__device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                         uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float bf16_half(uint32_t w, int which) {
+  return __uint_as_float(which ? w & 0xffff0000u : w << 16);
+}
+template <int N>
+__device__ __forceinline__ void lds_words(uint32_t addr, uint32_t* w) {
+  if constexpr (N == 4)
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr));
+  else if constexpr (N == 2)
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr));
+  else
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(addr));
+}
+
+template <int KIND, int D>
+struct Ring {
+  static constexpr bool kQ4 = KIND == HF_CACHE_Q4;
+  static constexpr int kKeys = kQ4 ? 32 : 16;            // keys of a warp's step
+  static constexpr int kRow = kQ4 ? D / 2 : 2 * D;       // bytes of a head-row
+  static constexpr int kScale = kQ4 ? D / 16 : 0;
+  static constexpr int kV = kKeys * kRow;                // offsets in a stage
+  static constexpr int kKs = 2 * kKeys * kRow;
+  static constexpr int kVs = kKs + kKeys * kScale;
+  static constexpr int kStage = kVs + kKeys * kScale;
+  static constexpr int kStages = kQ4 ? 4 : 3;            // D 128: 18 and 24 KB a warp
+  static constexpr int kWarpBytes = kStages * kStage;
+  static constexpr int kStep = kKeys * kWarps;           // keys of a block's step
+};
+
+// Byte of 16-byte chunk c of a key's row in a stage: where the reads of a warp
+// (ldmatrix: eight keys, one chunk; codes: see kappa) fall into different banks.
+template <int KIND, int D>
+__device__ __forceinline__ int chunk_at(int key, int c) {
+  if constexpr (KIND == HF_CACHE_Q4) {
+    constexpr int kPer = 128 / (D / 2);  // keys of a 128-byte line
+    const int line = key / kPer, at = (key % kPer) * (8 / kPer) + c;
+    return line * 128 + (at ^ ((line * kPer) & 6)) * 16;
+  } else {
+    return key * (2 * D) + (c ^ (key & 7)) * 16;
+  }
+}
+// Key of row r of S^T in a 16-key block of codes: rows 2 t, 2 t + 1 are keys t,
+// t + 4, so that the four lanes t read neighbouring rows of values.
+__device__ __forceinline__ int kappa(int r) { return (r & 8) + ((r & 7) >> 1) + 4 * (r & 1); }
+
+// Blocks on an SM: what the registers allow; rings of 72 and 96 KB a block.
+template <int KIND, int NT>
+constexpr int kBlocks = KIND == HF_CACHE_Q4 && NT == 1 ? 3 : 2;
+
+template <int KIND, int D, int NT>
+__global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
+    attend_rows_kernel(const CacheArgs C, const AttendArgs A) {
+  using R = Ring<KIND, D>;
+  constexpr bool kQ4 = R::kQ4;
+  constexpr int KB = R::kKeys, S = R::kStages;
+  constexpr int RB = 8 * NT;      // query rows of a unit
+  constexpr int NG = D / 32;
+  constexpr int kOut = D + 4;     // pitch of a query's outputs in shared memory
+  static_assert(RB * kOut * 4 <= R::kWarpBytes, "a warp's outputs fit its ring");
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int64_t s_pre[kMaxReq + 1];
+  __shared__ int64_t s_warp[kWarps];
+  __shared__ float s_m[kWarps][RB], s_l[kWarps][RB];
+  __shared__ int s_last;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = lane >> 2, t = lane & 3;
+  uint8_t* ring = smem + warp * R::kWarpBytes;
+  const uint32_t ring_a = smem_addr(ring);
+
+  // Steps of the sequences before each one.
+  {
+    int64_t carry = 0;
+    if (threadIdx.x == 0) s_pre[0] = 0;
+    for (int base = 0; base < C.n_seq; base += kThreads) {
+      const int i = base + threadIdx.x;
+      int64_t n = 0;
+      if (i < C.n_seq) {
+        const SeqSpan sp = seq_span(C, A, i);
+        const int64_t chunks = (static_cast<int64_t>(sp.n) * A.G + RB - 1) / RB;
+        n = chunks * C.H * max((sp.kv + R::kStep - 1) / R::kStep, 1);
+      }
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, n, o);
+        if (lane >= o) n += v;
+      }
+      if (lane == 31) s_warp[warp] = n;
+      __syncthreads();
+      int64_t add = carry;
+      for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) add += s_warp[w];
+        carry += s_warp[w];
+      }
+      if (i < C.n_seq) s_pre[i + 1] = n + add;
+      __syncthreads();
+    }
+  }
+  const int64_t total = s_pre[C.n_seq];
+  const int64_t n_cta = min(static_cast<int64_t>(gridDim.x), total);
+  const int64_t cta = blockIdx.x;
+  if (cta >= n_cta) return;
+  int64_t x = cta * total / n_cta;
+  const int64_t share0 = x, share1 = (cta + 1) * total / n_cta;
+
+  while (x < share1) {
+    // ---- the unit of step x, and this block's piece [p0, p1) of its steps
+    int lo = 0, hi = C.n_seq - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (s_pre[mid] <= x) lo = mid; else hi = mid - 1;
+    }
+    const int seq = lo;
+    const SeqSpan span = seq_span(C, A, seq);
+    const int chunks = static_cast<int>((static_cast<int64_t>(span.n) * A.G + RB - 1) / RB);
+    const int steps = max((span.kv + R::kStep - 1) / R::kStep, 1);
+    const int64_t unit = (x - s_pre[seq]) / steps;
+    const int64_t u0 = s_pre[seq] + unit * steps, u1 = u0 + steps;
+    const int h = static_cast<int>(unit / chunks), r0 = static_cast<int>(unit % chunks) * RB;
+    const int p0 = static_cast<int>(x - u0), p1 = static_cast<int>(min(share1, u1) - u0);
+    const int n_rows = static_cast<int>(min(static_cast<int64_t>(RB), static_cast<int64_t>(span.n) * A.G - r0));
+    const int kv_end = seen(span, A.causal, (r0 + n_rows - 1) / A.G);
+
+    // ---- queries
+    uint32_t qf[NT][D / 16][2];
+    float q_off[kQ4 ? NT : 1][kQ4 ? NG : 1][2];
+    int lim[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = 8 * nt + g;
+      const bool there = r < n_rows;
+      const __nv_bfloat16* q = nullptr;
+      if (there) {
+        const int rr = r0 + r;
+        q = reinterpret_cast<const __nv_bfloat16*>(A.q) + static_cast<int64_t>(span.first + rr / A.G) * A.q_row +
+            (h * A.G + rr % A.G) * A.q_head;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int rq = 8 * nt + 2 * t + e;
+        lim[nt][e] = rq < n_rows ? seen(span, A.causal, (r0 + rq) / A.G) : 0;
+      }
+      if constexpr (kQ4) {
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) {
+          uint4 u = make_uint4(0, 0, 0, 0);
+          if (there) u = *reinterpret_cast<const uint4*>(q + 32 * gr + 8 * t);
+          const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+          float f[8], sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            f[i] = bf16_half(w[i / 2], i & 1);
+            sum += f[i];
+          }
+          const float b = 18446744073709551616.f, b16 = 1152921504606846976.f;  // 2^64, 2^60
+          qf[nt][2 * gr][0] = pack_bf16(f[0] * b, f[4] * b);
+          qf[nt][2 * gr][1] = pack_bf16(f[2] * b, f[6] * b);
+          qf[nt][2 * gr + 1][0] = pack_bf16(f[1] * b16, f[5] * b16);
+          qf[nt][2 * gr + 1][1] = pack_bf16(f[3] * b16, f[7] * b16);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+          sum *= -8.f * 1.6940658945086007e-21f;  // 2^-69
+          q_off[nt][gr][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
+          q_off[nt][gr][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          qf[nt][i][0] = there ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 2 * t) : 0u;
+          qf[nt][i][1] = there ? *reinterpret_cast<const uint32_t*>(q + 16 * i + 8 + 2 * t) : 0u;
+        }
+      }
+    }
+    const float scale = kQ4 ? A.scale_log2 * 590295810358705651712.f : A.scale_log2;  // 2^69
+
+    // ---- the warp's ring
+    const char* kb = C.k + (kQ4 ? static_cast<int64_t>(h) * C.rows * (D / 2) : h * C.head_stride * 2);
+    const char* vb = C.v + (kQ4 ? static_cast<int64_t>(h) * C.rows * (D / 2) : h * C.head_stride * 2);
+    const int64_t row_bytes = kQ4 ? D / 2 : C.row_stride * 2;
+    const char* ksb = C.ks + static_cast<int64_t>(h) * C.rows * (D / 16);
+    const char* vsb = C.vs + static_cast<int64_t>(h) * C.rows * (D / 16);
+    auto row_of = [&](int step) -> int {  // of key `lane` of this warp's step
+      const int key = step * R::kStep + warp * KB + lane;
+      return step < p1 && lane < KB && key < kv_end ? cache_row(C, seq, key) : -1;
+    };
+    auto issue = [&](int step, int stage, int row) {
+      if (step < p1) {
+        const uint32_t dst = ring_a + stage * R::kStage;
+        constexpr int kChunks = R::kRow / 16;
+#pragma unroll
+        for (int i = 0; i < KB * kChunks / 32; ++i) {
+          const int idx = i * 32 + lane, key = idx / kChunks, c = idx % kChunks;
+          const int r = __shfl_sync(0xffffffffu, row, key);
+          const int64_t at = max(r, 0) * row_bytes + c * 16;
+          const uint32_t d = dst + chunk_at<KIND, D>(key, c);
+          cp_async_16_or_zero(d, kb + at, r >= 0);
+          cp_async_16_or_zero(d + R::kV, vb + at, r >= 0);
+        }
+        if constexpr (kQ4) {
+          const int64_t at = static_cast<int64_t>(max(row, 0)) * R::kScale;
+          cp_async_small<R::kScale>(dst + R::kKs + lane * R::kScale, ksb + at, row >= 0);
+          cp_async_small<R::kScale>(dst + R::kVs + lane * R::kScale, vsb + at, row >= 0);
+        }
+      }
+      cp_async_commit();
+    };
+
+    float o[NT][D / 16][4], o_off[kQ4 ? NT : 1][kQ4 ? NG : 1][4];
+    float m[NT][2], l[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
+      if constexpr (kQ4) {
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o_off[nt][i][e] = 0.f;
+      }
+      m[nt][0] = m[nt][1] = -INFINITY;
+      l[nt][0] = l[nt][1] = 0.f;
+    }
+
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) issue(p0 + i, i, row_of(p0 + i));
+    int row = row_of(p0 + S - 1);
+    int stage = 0, ahead = S - 1;
+    for (int step = p0; step < p1; ++step) {
+      cp_async_wait<S - 2>();
+      __syncwarp();  // the stage is everybody's, and the one before it is read
+      issue(step + S - 1, ahead, row);
+      row = row_of(step + S);
+      const uint32_t st = ring_a + stage * R::kStage;
+      if (++stage == S) stage = 0;
+      if (++ahead == S) ahead = 0;
+      const int key0 = step * R::kStep + warp * KB;
+      if (key0 >= kv_end) continue;
+#pragma unroll
+      for (int b = 0; b < KB / 16; ++b) {
+        // scores
+        float s[NT][4];
+        uint32_t vs[2][kQ4 ? (NG + 1) / 2 : 1];  // scales of the values of keys kappa(g), kappa(g + 8)
+        if constexpr (kQ4) {
+          uint32_t w[2][NG], sc[2][(NG + 1) / 2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int key = 16 * b + kappa(g + 8 * e);
+            if constexpr (NG == 4)
+              lds_words<4>(st + chunk_at<KIND, D>(key, t), w[e]);
+            else
+              lds_words<2>(st + chunk_at<KIND, D>(key, t >> 1) + 8 * (t & 1), w[e]);
+            lds_words<NG / 2>(st + R::kKs + key * R::kScale, sc[e]);
+            lds_words<NG / 2>(st + R::kVs + key * R::kScale, vs[e]);
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
+#pragma unroll
+          for (int gr = 0; gr < NG; ++gr) {
+            uint32_t c8[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              c8[e] = __byte_perm(w[e][gr / 2], w[e][NG / 2 + gr / 2], gr & 1 ? 0x7632 : 0x5410);
+            const uint32_t d8[2] = {c8[0] >> 8, c8[1] >> 8};
+            const float f0 = bf16_half(sc[0][gr / 2], gr & 1), f1 = bf16_half(sc[1][gr / 2], gr & 1);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              float c[4] = {q_off[nt][gr][0], q_off[nt][gr][1], q_off[nt][gr][0], q_off[nt][gr][1]};
+              mma16816(c, c8[0] & 0x000f000fu, c8[1] & 0x000f000fu, d8[0] & 0x000f000fu, d8[1] & 0x000f000fu,
+                       qf[nt][2 * gr][0], qf[nt][2 * gr][1]);
+              mma16816(c, c8[0] & 0x00f000f0u, c8[1] & 0x00f000f0u, d8[0] & 0x00f000f0u, d8[1] & 0x00f000f0u,
+                       qf[nt][2 * gr + 1][0], qf[nt][2 * gr + 1][1]);
+              s[nt][0] = fmaf(f0, c[0], s[nt][0]);
+              s[nt][1] = fmaf(f0, c[1], s[nt][1]);
+              s[nt][2] = fmaf(f1, c[2], s[nt][2]);
+              s[nt][3] = fmaf(f1, c[3], s[nt][3]);
+            }
+          }
+        } else {
+          float s2[NT][4];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[nt][e] = s2[nt][e] = 0.f;
+          const int key = 16 * b + (lane & 7) + (lane & 8);
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            uint32_t a[4];
+            ldmatrix4(st + chunk_at<KIND, D>(key, 2 * i + (lane >> 4)), a);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              mma16816(i & 1 ? s2[nt] : s[nt], a[0], a[1], a[2], a[3], qf[nt][i][0], qf[nt][i][1]);
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[nt][e] += s2[nt][e];
+        }
+        // what is not seen, and the running maximum
+        const int ka = key0 + 16 * b + (kQ4 ? kappa(g) : g), kb8 = ka + 8;
+        bool past = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[nt][e] = (e < 2 ? ka : kb8) < lim[nt][e & 1] ? s[nt][e] * scale : -INFINITY;
+            past |= s[nt][e] > m[nt][e & 1] + kStretch;
+          }
+        if (__any_sync(0xffffffffu, past)) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float top = fmaxf(s[nt][e], s[nt][e + 2]);
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+              const float next = fmaxf(m[nt][e], top);
+              const float fix = next == -INFINITY ? 1.f : exp2_approx(m[nt][e] - next);
+              m[nt][e] = next;
+              l[nt][e] *= fix;
+#pragma unroll
+              for (int i = 0; i < D / 16; ++i) {
+                o[nt][i][e] *= fix;
+                o[nt][i][e + 2] *= fix;
+              }
+              if constexpr (kQ4) {
+#pragma unroll
+                for (int i = 0; i < NG; ++i) {
+                  o_off[nt][i][e] *= fix;
+                  o_off[nt][i][e + 2] *= fix;
+                }
+              }
+            }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float top = m[nt][e & 1];
+            s[nt][e] = exp2_approx(s[nt][e] - (top == -INFINITY ? 0.f : top));
+            l[nt][e & 1] += s[nt][e];
+          }
+        // outputs
+        if constexpr (kQ4) {
+          uint32_t w[4][(NG + 1) / 2];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)  // keys t, t + 4, t + 8, t + 12: rows 2 t, 2 t + 1, ... of S^T
+            if constexpr (NG == 4)
+              lds_words<2>(st + R::kV + chunk_at<KIND, D>(16 * b + t + 4 * e, g >> 1) + 8 * (g & 1), w[e]);
+            else
+              lds_words<1>(st + R::kV + chunk_at<KIND, D>(16 * b + t + 4 * e, g >> 2) + 4 * (g & 3), w[e]);
+#pragma unroll
+          for (int gr = 0; gr < NG; ++gr) {
+            const float b64 = 18446744073709551616.f;  // 2^64
+            const float f0 = bf16_half(vs[0][gr / 2], gr & 1) * b64, f1 = bf16_half(vs[1][gr / 2], gr & 1) * b64;
+            const uint32_t c8 = __byte_perm(w[0][gr / 2], w[1][gr / 2], gr & 1 ? 0x7632 : 0x5410);
+            const uint32_t e8 = __byte_perm(w[2][gr / 2], w[3][gr / 2], gr & 1 ? 0x7632 : 0x5410);
+            const uint32_t d8 = c8 >> 8, g8 = e8 >> 8;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              const uint32_t b0 = movmatrix_trans(pack_bf16(s[nt][0] * f0, s[nt][1] * f0));
+              const uint32_t b1 = movmatrix_trans(pack_bf16(s[nt][2] * f1, s[nt][3] * f1));
+              mma16816(o[nt][2 * gr], c8 & 0x000f000fu, d8 & 0x000f000fu, e8 & 0x000f000fu, g8 & 0x000f000fu, b0, b1);
+              mma16816(o[nt][2 * gr + 1], c8 & 0x00f000f0u, d8 & 0x00f000f0u, e8 & 0x00f000f0u, g8 & 0x00f000f0u, b0,
+                       b1);
+              mma16816(o_off[nt][gr], 0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u, b0, b1);
+            }
+          }
+        } else {
+          uint32_t pb[NT][2];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            pb[nt][0] = movmatrix_trans(pack_bf16(s[nt][0], s[nt][1]));
+            pb[nt][1] = movmatrix_trans(pack_bf16(s[nt][2], s[nt][3]));
+          }
+          const int key = 16 * b + (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            uint32_t a[4];
+            ldmatrix4_trans(st + R::kV + chunk_at<KIND, D>(key, 2 * i + ((lane >> 3) & 1)), a);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              mma16816(o[nt][i], a[0], a[1], a[2], a[3], pb[nt][0], pb[nt][1]);
+          }
+        }
+      }
+    }
+    cp_async_wait<0>();
+    __syncwarp();
+
+    // ---- the warps' results side by side in shared memory
+    float* so = reinterpret_cast<float*>(ring);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float sum = l[nt][e];
+        sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+        const int q = 8 * nt + 2 * t + e;
+        if (g == 0) {
+          s_m[warp][q] = m[nt][e];
+          s_l[warp][q] = sum;
+        }
+        float* dst = so + q * kOut;
+        if constexpr (kQ4) {
+          const float back = 590295810358705651712.f;  // 2^69
+#pragma unroll
+          for (int gr = 0; gr < NG; ++gr) {
+            const float off = o_off[nt][gr][e];
+            dst[32 * gr + 4 * g] = (o[nt][2 * gr][e] - off) * back;
+            dst[32 * gr + 4 * g + 2] = (o[nt][2 * gr][e + 2] - off) * back;
+            dst[32 * gr + 4 * g + 1] = (o[nt][2 * gr + 1][e] * 0.0625f - off) * back;
+            dst[32 * gr + 4 * g + 3] = (o[nt][2 * gr + 1][e + 2] * 0.0625f - off) * back;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            dst[16 * i + g] = o[nt][i][e];
+            dst[16 * i + g + 8] = o[nt][i][e + 2];
+          }
+        }
+      }
+    }
+    __syncthreads();
+
+    const bool whole = p0 == 0 && p1 == steps;
+    // A unit's pieces lie in blocks c0 .. c1; a block's first piece is its slot 0,
+    // another one that it shares its slot 1.
+    const int64_t c0 = ((u0 + 1) * n_cta - 1) / total, c1 = (u1 * n_cta - 1) / total;
+    const int64_t slot = 2 * cta + (x == share0 ? 0 : 1);
+    for (int i = threadIdx.x; i < n_rows * (D / 4); i += kThreads) {
+      const int q = i / (D / 4), c = i % (D / 4) * 4;
+      float top = s_m[0][q];
+#pragma unroll
+      for (int w = 1; w < kWarps; ++w) top = fmaxf(top, s_m[w][q]);
+      const float base = top == -INFINITY ? 0.f : top;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = exp2_approx(s_m[w][q] - base);
+        const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem + w * R::kWarpBytes) +
+                                                          q * kOut + c);
+        sum = fmaf(s_l[w][q], f, sum);
+        acc.x = fmaf(v.x, f, acc.x);
+        acc.y = fmaf(v.y, f, acc.y);
+        acc.z = fmaf(v.z, f, acc.z);
+        acc.w = fmaf(v.w, f, acc.w);
+      }
+      if (whole) {
+        const int rr = r0 + q;
+        const int64_t tok = span.first + rr / A.G;
+        const int hq = h * A.G + rr % A.G;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(A.out) + tok * A.o_row + hq * A.o_head + c;
+        *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+        if (A.lse && c == 0) A.lse[tok * A.H_q + hq] = (top + log2f(sum)) * 0.693147180559945309f;
+      } else {
+        const int64_t at = slot * RB + q;
+        *reinterpret_cast<float4*>(A.part_o + at * D + c) = acc;
+        if (c == 0) A.part_ml[at] = make_float2(top, sum);
+      }
+    }
+    if (!whole) {
+      // the last block at the unit joins its pieces, in the blocks' order
+      __threadfence();
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        const int done = atomicAdd(A.zeroed + c0, 1);
+        s_last = done == static_cast<int>(c1 - c0);
+        if (s_last) A.zeroed[c0] = 0;
+        __threadfence();
+      }
+      __syncthreads();
+      if (s_last) {
+        for (int i = threadIdx.x; i < n_rows * (D / 4); i += kThreads) {
+          const int q = i / (D / 4), c = i % (D / 4) * 4;
+          const int64_t first = 2 * c0 + (c0 * total / n_cta == u0 ? 0 : 1);
+          float top = -INFINITY;
+          for (int64_t b = c0; b <= c1; ++b) top = fmaxf(top, __ldcg(&A.part_ml[(b == c0 ? first : 2 * b) * RB + q]).x);
+          const float base = top == -INFINITY ? 0.f : top;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          float sum = 0.f;
+#pragma unroll 4
+          for (int64_t b = c0; b <= c1; ++b) {
+            const int64_t at = (b == c0 ? first : 2 * b) * RB + q;
+            const float2 ml = __ldcg(&A.part_ml[at]);
+            const float f = exp2_approx(ml.x - base);
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(A.part_o + at * D + c));
+            sum = fmaf(ml.y, f, sum);
+            acc.x = fmaf(v.x, f, acc.x);
+            acc.y = fmaf(v.y, f, acc.y);
+            acc.z = fmaf(v.z, f, acc.z);
+            acc.w = fmaf(v.w, f, acc.w);
+          }
+          const int rr = r0 + q;
+          const int64_t tok = span.first + rr / A.G;
+          const int hq = h * A.G + rr % A.G;
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(A.out) + tok * A.o_row + hq * A.o_head + c;
+          *reinterpret_cast<uint2*>(dst) =
+              make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+          if (A.lse && c == 0) A.lse[tok * A.H_q + hq] = (top + log2f(sum)) * 0.693147180559945309f;
+        }
+      }
+    }
+    __syncthreads();  // the rings and s_m are free again
+    x = u0 + p1;
+  }
+}
+
+template <int KIND, int D, int NT>
+hf_status launch_rows(const CacheArgs& c, const AttendArgs& a, cudaStream_t stream) {
+  auto kern = attend_rows_kernel<KIND, D, NT>;
+  constexpr int smem = Ring<KIND, D>::kWarpBytes * kWarps;
+  HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem),
+              "hf_attend: shared memory size");
+  kern<<<device_sm_count() * kBlocks<KIND, NT>, kThreads, smem, stream>>>(c, a);
+  HF_CUDA_TRY(cudaGetLastError(), "hf_attend: launch");
+  return HF_OK;
+}
+
+}  // namespace
+
+bool attend_rows_takes(hf_cache_kind kind, hf_dtype dtype, int D) {
+  return dtype == HF_BF16 && kind != HF_CACHE_F32 && (D == 64 || D == 128);
+}
+
+hf_status attend_rows(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_rows, cudaStream_t stream) {
+  const bool one = max_rows <= 8;
+  if (kind == HF_CACHE_Q4) {
+    if (c.D == 64)
+      return one ? launch_rows<HF_CACHE_Q4, 64, 1>(c, a, stream) : launch_rows<HF_CACHE_Q4, 64, 2>(c, a, stream);
+    return one ? launch_rows<HF_CACHE_Q4, 128, 1>(c, a, stream) : launch_rows<HF_CACHE_Q4, 128, 2>(c, a, stream);
+  }
+  if (c.D == 64)
+    return one ? launch_rows<HF_CACHE_BF16, 64, 1>(c, a, stream) : launch_rows<HF_CACHE_BF16, 64, 2>(c, a, stream);
+  return one ? launch_rows<HF_CACHE_BF16, 128, 1>(c, a, stream) : launch_rows<HF_CACHE_BF16, 128, 2>(c, a, stream);
+}
+
+}  // namespace hf
