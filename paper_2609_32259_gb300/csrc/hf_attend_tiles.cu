@@ -1,0 +1,491 @@
+// Attention of many query rows: prompts, and questions behind a long context.
+//
+//   S = Q K^T,  P = 2^(scale log2(e) S - m),  O += P V,  out = O / sum(P)
+//
+// Bound by the tensor cores: 4 D FLOP for every visible (query row, key) pair. A
+// block owns 256 flattened query rows of one KV head (two tiles of 128) and walks
+// its keys 128 at a time; the two tiles take turns on the tensor core, so that
+// one's softmax runs under the other's products.
+//
+//   warps 0-3, 4-7  softmax of tile 0 and 1: a thread a row.  Scores come from
+//                   tensor memory, probabilities go back there as bf16 over them,
+//                   as the next product's first operand.  The running maximum
+//                   moves only when a score passes it by 2^8; the outputs in tensor
+//                   memory are rescaled then, by the same thread.
+//   warps 8-11      loaders: Q once, then K and V tiles, rows looked up page by
+//                   page, by cp.async into the 128-byte-swizzled layout; a 4-bit
+//                   cache's codes are expanded to bf16 (exactly) on the way.
+//   warp 12         issues the products: S_i = Q_i K^T from shared memory, O_i +=
+//                   P_i V with P_i in tensor memory and V as it lies (its
+//                   channels contiguous).
+// Tensor memory: S0, S1 (P over them) and O0, O1, 128 columns each.  The
+// products of one tile follow each other in issue order, so a tile's new scores
+// also say that its last product with V is done.
+//
+// Every wait is bounded; one that runs out sets HF_CHECK_TIMEOUT and ends the
+// block.
+#include <algorithm>
+
+#include "hf_attend.cuh"
+
+namespace hf {
+namespace {
+
+constexpr int kTile = 128;       // query rows of a tile, keys of a step
+constexpr int kThreads = 512;    // 13 warps work; registers are shared out by warpgroup
+constexpr float kStretch = 8.f;  // log2 of what a score may pass the running maximum by
+
+__device__ __forceinline__ void cp_async_16_or_zero(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void regs_more() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_less() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// D[tmem] (+)= A[tmem] * B[smem]
+__device__ __forceinline__ void mma_bf16_tmem_a(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                                uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// Descriptor of an operand whose rows (K) are 128-byte pieces of the other
+// dimension, 128-byte swizzle: 1,024 bytes from eight rows of K to the next
+// eight, `pitch` bytes from 64 values of the other dimension to the next.
+__device__ __forceinline__ uint64_t sw128_mnmajor_desc(uint32_t saddr, uint32_t pitch) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(pitch >> 4) << 16) |
+         (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) |
+         (static_cast<uint64_t>(2) << 61);
+}
+
+// mbar_wait without a call: the registers of a kernel that shares them out anew
+// (setmaxnreg) cannot be allocated around one.
+__device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = global_timer_ns();
+  for (uint32_t i = 1;; ++i) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((i & 63u) == 0 && global_timer_ns() - t0 > kWaitLimitNs) return false;
+  }
+}
+
+#define HF_R4(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3])
+#define HF_W4(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3])
+// 32 columns of this thread's lane.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : HF_R4(r, 0), HF_R4(r, 4), HF_R4(r, 8), HF_R4(r, 12), HF_R4(r, 16), HF_R4(r, 20), HF_R4(r, 24), HF_R4(r, 28)
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15};" ::HF_W4(r, 0),
+      HF_W4(r, 4), HF_W4(r, 8), HF_W4(r, 12), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Waits for this warp's loads; the registers pass through, so that no use moves above.
+#define HF_P4(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3])
+__device__ __forceinline__ void tmem_ld_wait32(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : HF_P4(r, 0), HF_P4(r, 4), HF_P4(r, 8), HF_P4(r, 12), HF_P4(r, 16), HF_P4(r, 20), HF_P4(r, 24),
+                 HF_P4(r, 28)::"memory");
+}
+
+template <int D>
+struct Smem {
+  static constexpr int kPart = kTile * 128;           // 128 rows of 64 channels
+  static constexpr int kOperand = kPart * (D / 64);   // a tile of Q, K or V
+  static constexpr int kStages = D == 128 ? 5 : 6;
+  static constexpr int kQ = 0;
+  static constexpr int kKV = 2 * kOperand;
+  static constexpr int kBars = kKV + kStages * kOperand;
+  static constexpr int kBytes = kBars + 256;
+};
+
+template <int KIND, int D>
+__global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheArgs C, const AttendArgs A, int ns) {
+  using M = Smem<D>;
+  constexpr int S = M::kStages;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  // ---- the block's rows and keys
+  const int h = blockIdx.x % C.H, sp = blockIdx.y;
+  const TilePlace place = find_tile(C, A, 2 * kTile, blockIdx.x / C.H);
+  if (place.seq >= C.n_seq) return;
+  const SeqSpan span = seq_span(C, A, place.seq);
+  const int r0 = (place.tiles - 1 - place.at) * 2 * kTile;  // the longest first
+  const int n_rows = static_cast<int>(min(static_cast<int64_t>(2 * kTile), static_cast<int64_t>(span.n) * A.G - r0));
+  // keys of this part: tiles [t0, t1) of 128; of query tile i: up to its last row's
+  const int kv_end = seen(span, A.causal, (r0 + n_rows - 1) / A.G);
+  const int all = (kv_end + kTile - 1) / kTile;
+  const int t0 = static_cast<int>(static_cast<int64_t>(all) * sp / ns);
+  const int t1 = static_cast<int>(static_cast<int64_t>(all) * (sp + 1) / ns);
+  int nt[2];
+  {
+    const int last0 = min(n_rows, kTile) - 1;
+    const int end0 = seen(span, A.causal, (r0 + last0) / A.G);
+    nt[0] = max(min((end0 + kTile - 1) / kTile, t1) - t0, 0);
+    nt[1] = n_rows > kTile ? t1 - t0 : 0;
+  }
+  const int n_max = max(nt[0], nt[1]);
+
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + M::kBars);
+  const uint32_t full = smem_addr(bars), empty = full + 8 * S, qfull = empty + 8 * S, sfull = qfull + 8,
+                 pfull = sfull + 16, ofull = pfull + 16, drain = ofull + 16;
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + M::kBars + 8 * (2 * S + 8));
+  if (smem_addr(smem) & 1023u) {
+    if (threadIdx.x == 0) set_status(C, HF_CHECK_INTERNAL);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(full + 8 * s, 4);
+      mbar_init(empty + 8 * s, 1);
+    }
+    mbar_init(qfull, 4);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(sfull + 8 * i, 1);
+      mbar_init(pfull + 8 * i, 4);
+      mbar_init(ofull + 8 * i, 1);
+    }
+    mbar_init(drain, 1);
+    fence_barrier_init();
+  }
+  if (warp == 12) {
+    tmem_alloc(smem_addr(s_tmem), 512);
+    tmem_relinquish();
+  }
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *s_tmem;
+  auto timed_out = [&]() { set_status(C, HF_CHECK_TIMEOUT); };
+
+  // Registers, by warpgroup: 2 x 200 + 72 + 40 = 4 x 128.
+  if (warp < 8) {
+    // ------------------------------------------------------------ softmax
+    regs_more<200>();
+    const int i = warp >> 2;
+    const int row = (warp & 3) * 32 + lane;
+    const int rr = r0 + i * kTile + row;
+    const bool live = i * kTile + row < n_rows;
+    const int lim = live ? seen(span, A.causal, rr / A.G) : 0;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t ts = tmem + i * 128 + lanes, to = tmem + 256 + i * 128 + lanes;
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    const int n = nt[i];
+    for (int j = 0; j < n; ++j) {
+      if (!wait_here(sfull + 8 * i, j & 1)) {
+        timed_out();
+        ok = false;
+        break;
+      }
+      tc_fence_after_sync();
+      uint32_t s[128];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32(ts + 32 * c, s + 32 * c);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld_wait32(s + 32 * c);
+      const int vis = lim - (t0 + j) * kTile;  // columns that this row sees
+      if (__any_sync(0xffffffffu, vis < kTile)) {
+#pragma unroll
+        for (int c = 0; c < 128; ++c)
+          if (c >= vis) s[c] = 0xff800000u;
+      }
+      float top = __uint_as_float(s[0]);
+#pragma unroll
+      for (int c = 1; c < 128; ++c) top = fmaxf(top, __uint_as_float(s[c]));
+      top *= A.scale_log2;
+      if (__any_sync(0xffffffffu, top > m + kStretch)) {
+        const float next = top > m + kStretch ? top : m;
+        const float fix = next == m ? 1.f : exp2_approx(m - next);
+        m = next;
+        l *= fix;
+        if (j > 0) {
+#pragma unroll
+          for (int c = 0; c < D; c += 16) {
+            uint32_t o[16];
+            tmem_load_16(to + c, o);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fix);
+            tmem_st16(to + c, o);
+          }
+        }
+      }
+      const float base = m == -INFINITY ? 0.f : -m;
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < 128; c += 32) {
+        uint32_t p[16];
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+          const float a = exp2_approx(fmaf(__uint_as_float(s[c + e]), A.scale_log2, base));
+          const float b = exp2_approx(fmaf(__uint_as_float(s[c + e + 1]), A.scale_log2, base));
+          sum[e / 2 % 4] += a + b;
+          p[e / 2] = pack_bf16(a, b);
+        }
+        tmem_st16(ts + c / 2, p);
+      }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tmem_st_wait();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(pfull + 8 * i);
+    }
+    // ---- outputs
+    const int64_t tok = span.first + rr / A.G;
+    const int hq = h * A.G + rr % A.G;
+    if (ok && n > 0 && !wait_here(ofull + 8 * i, 0)) {
+      timed_out();
+      ok = false;
+    }
+    if (ok) {
+      tc_fence_after_sync();
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int64_t slot = (static_cast<int64_t>(sp) * A.n_tok + tok) * A.H_q + hq;
+#pragma unroll
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32];
+        if (n > 0) {
+          tmem_ld32(to + c, o);
+          tmem_ld_wait32(o);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0u;
+        }
+        if (live) {
+          if (ns > 1) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              *reinterpret_cast<uint4*>(A.part_o + slot * D + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          } else {
+            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(A.out) + tok * A.o_row + hq * A.o_head + c;
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) {
+              uint32_t w[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                w[k] = pack_bf16(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
+              *reinterpret_cast<uint4*>(dst + e) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+        }
+      }
+      if (live) {
+        if (ns > 1)
+          A.part_ml[slot] = make_float2(m, l);
+        else if (A.lse)
+          A.lse[tok * A.H_q + hq] = (m + log2f(l)) * 0.693147180559945309f;
+      }
+    }
+  } else if (warp < 12) {
+    // ------------------------------------------------------------ loaders
+    regs_less<72>();
+    const int w = warp - 8;
+    constexpr int kChunks = D / 8;  // 16-byte pieces of a row
+    {
+      // a lane's rows of Q: 32 (w + 4 k) + lane, k < 2
+#pragma unroll 1
+      for (int k = 0; k < 2; ++k) {
+        int64_t at = -1;
+        const int row = 32 * (w + 4 * k) + lane;
+        if (row < n_rows) {
+          const int rr = r0 + row;
+          at = static_cast<int64_t>(span.first + rr / A.G) * A.q_row + (h * A.G + rr % A.G) * A.q_head;
+        }
+#pragma unroll 4
+        for (int x = 0; x < kChunks; ++x) {
+          const int idx = x * 32 + lane, c = idx % kChunks, src = idx / kChunks;
+          const int64_t a = __shfl_sync(0xffffffffu, at, src);
+          const int qr = 32 * w + src;  // row in its tile
+          const uint32_t dst = smem_addr(smem) + M::kQ + k * M::kOperand + (c / 8) * M::kPart + qr * 128 +
+                               (((c % 8) ^ (qr & 7)) << 4);
+          cp_async_16_or_zero(dst, A.q + (a < 0 ? 0 : a * 2 + c * 16), a >= 0);
+        }
+      }
+      cp_async_commit();
+    }
+    const char* kb = C.k + h * C.head_stride * 2;
+    const char* vb = C.v + h * C.head_stride * 2;
+    constexpr int kLag = 2;
+    const int n = 2 * n_max;
+    bool ok = true;
+    int stage = 0, done = 0;
+    uint32_t phase = 1;
+    int row = -1;
+    for (int x = 0; x < n + kLag && ok; ++x) {
+      if (x < n) {
+        if (!wait_here(empty + 8 * stage, phase)) {
+          timed_out();
+          ok = false;
+          break;
+        }
+        if ((x & 1) == 0) {
+          const int key = (t0 + (x >> 1)) * kTile + 32 * w + lane;
+          row = key < kv_end ? cache_row(C, place.seq, key) : -1;
+        }
+        const char* src = x & 1 ? vb : kb;
+        const uint32_t base = smem_addr(smem) + M::kKV + stage * M::kOperand;
+#pragma unroll 4
+        for (int y = 0; y < kChunks; ++y) {
+          const int idx = y * 32 + lane, c = idx % kChunks, kr = idx / kChunks;
+          const int r = __shfl_sync(0xffffffffu, row, kr);
+          const int key = 32 * w + kr;
+          cp_async_16_or_zero(base + (c / 8) * M::kPart + key * 128 + (((c % 8) ^ (key & 7)) << 4),
+                              src + max(r, 0) * (C.row_stride * 2) + c * 16, r >= 0);
+        }
+        if (++stage == S) {
+          stage = 0;
+          phase ^= 1;
+        }
+      }
+      cp_async_commit();
+      // what was issued kLag steps ago (before the first tile: Q) has arrived
+      cp_async_wait<kLag>();
+      if (x >= kLag) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if (x == kLag) mbar_arrive(qfull);
+          mbar_arrive(full + 8 * done);
+        }
+        if (++done == S) done = 0;
+      }
+    }
+    if (ok && n == 0) {
+      cp_async_wait<0>();
+    }
+  } else {
+    // ------------------------------------------------------------ products
+    regs_less<40>();
+    if (warp == 12 && lane == 0 && n_max > 0) {
+      constexpr uint32_t idesc_s = make_idesc(1u, kTile, kTile);
+      constexpr uint32_t idesc_o = make_idesc(1u, kTile, D) | (1u << 16);
+      const uint32_t kv0 = smem_addr(smem) + M::kKV;
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      auto step = [&](int* s, uint32_t* p) {  // the next stage
+        *s = stage, *p = phase;
+        if (++stage == S) {
+          stage = 0;
+          phase ^= 1;
+        }
+      };
+      auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (ok && !wait_here(bar, parity)) {
+          timed_out();
+          ok = false;
+        }
+        return ok;
+      };
+      auto scores = [&](int i, int ks) {
+        const uint64_t a = sw128_kmajor_desc(smem_addr(smem) + M::kQ + i * M::kOperand);
+        const uint64_t b = sw128_kmajor_desc(kv0 + ks * M::kOperand);
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+          const uint64_t off = ((c / 4) * M::kPart + (c % 4) * 32) >> 4;
+          mma_bf16(tmem + i * 128, a + off, b + off, idesc_s, c > 0);
+        }
+        tc_commit(sfull + 8 * i);
+      };
+      int ks = 0, vs = 0;
+      uint32_t kp = 0, vp = 0;
+      step(&ks, &kp);
+      if (wait(qfull, 0) && wait(full + 8 * ks, kp)) {
+        tc_fence_after_sync();
+        for (int i = 0; i < 2; ++i)
+          if (nt[i] > 0) scores(i, ks);
+        tc_commit(empty + 8 * ks);
+      }
+      for (int j = 0; j < n_max && ok; ++j) {
+        step(&vs, &vp);
+        if (!wait(full + 8 * vs, vp)) break;
+        const bool more = j + 1 < n_max;
+        if (more) step(&ks, &kp);
+        for (int i = 0; i < 2 && ok; ++i) {
+          if (j < nt[i]) {
+            if (!wait(pfull + 8 * i, j & 1)) break;
+            tc_fence_after_sync();
+            const uint64_t b = sw128_mnmajor_desc(kv0 + vs * M::kOperand, M::kPart);
+#pragma unroll
+            for (int c = 0; c < kTile / 16; ++c)
+              mma_bf16_tmem_a(tmem + 256 + i * 128, tmem + i * 128 + 8 * c, b + ((c * 2048) >> 4), idesc_o,
+                              j > 0 || c > 0);
+            if (j + 1 == nt[i]) tc_commit(ofull + 8 * i);
+          }
+          if (i == 1) tc_commit(empty + 8 * vs);
+          if (more) {
+            if (i == 0 && !wait(full + 8 * ks, kp)) break;
+            if (i == 0) tc_fence_after_sync();
+            if (j + 1 < nt[i]) scores(i, ks);
+          }
+        }
+        if (more && ok) tc_commit(empty + 8 * ks);
+      }
+      tc_commit(drain);
+      if (!wait_here(drain, 0)) timed_out();
+    }
+    __syncwarp();
+  }
+  __syncthreads();
+  if (warp == 12) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int KIND, int D>
+hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int max_kv, cudaStream_t stream) {
+  const int64_t tiles = most_tiles(a.n_tok, a.G, c.n_seq, 2 * kTile) * c.H;
+  // keys are split where the tiles leave SMs idle, in parts of 512 keys at least,
+  // as far as the workspace goes
+  int64_t ns = std::min<int64_t>(device_sm_count() / tiles, (max_kv + 511) / 512);
+  ns = std::min<int64_t>(ns, part_rows(device_sm_count()) / (static_cast<int64_t>(a.n_tok) * a.H_q));
+  ns = std::max<int64_t>(1, std::min<int64_t>(ns, 64));
+  auto kern = attend_tiles_kernel<KIND, D>;
+  HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::kBytes),
+              "hf_attend: shared memory size");
+  kern<<<dim3(static_cast<unsigned>(tiles), static_cast<unsigned>(ns)), kThreads, Smem<D>::kBytes, stream>>>(
+      c, a, static_cast<int>(ns));
+  HF_CUDA_TRY(cudaGetLastError(), "hf_attend: launch");
+  if (ns > 1) return launch_join(HF_BF16, D, a, static_cast<int>(ns), stream);
+  return HF_OK;
+}
+
+}  // namespace
+
+bool attend_tiles_takes(hf_cache_kind kind, hf_dtype dtype, int D) {
+  return dtype == HF_BF16 && kind == HF_CACHE_BF16 && (D == 64 || D == 128);
+}
+
+hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_kv, cudaStream_t stream) {
+  (void)kind;
+  if (c.D == 64) return launch_tiles<HF_CACHE_BF16, 64>(c, a, max_kv, stream);
+  return launch_tiles<HF_CACHE_BF16, 128>(c, a, max_kv, stream);
+}
+
+}  // namespace hf
