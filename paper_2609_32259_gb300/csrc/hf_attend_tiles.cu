@@ -113,6 +113,63 @@ __device__ __forceinline__ void tmem_ld_wait32(uint32_t* r) {
                  HF_P4(r, 28)::"memory");
 }
 
+// Eight channels of a 4-bit row lie in an operand as their codes do in a word:
+// 0 4 1 5 2 6 3 7; channel k is at place code_place(k).
+__host__ __device__ constexpr int code_place(int k) { return k < 4 ? 2 * k : 2 * k - 7; }
+
+// This lane's codes and scales of a row (lane m of the row's four).
+template <int D>
+struct Q4Words {
+  uint32_t w[D / 32], s[D / 64];
+};
+template <int D>
+__device__ __forceinline__ void load_q4(Q4Words<D>& q, const char* codes, const char* scales, int row, int m) {
+  constexpr int NG = D / 32;
+  if (row < 0) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) q.w[i] = 0u;
+#pragma unroll
+    for (int i = 0; i < NG / 2; ++i) q.s[i] = 0u;
+    return;
+  }
+  const int64_t r = row;
+  if constexpr (D == 128) {
+    const uint4 u = *reinterpret_cast<const uint4*>(codes + r * 64 + m * 16);
+    q.w[0] = u.x, q.w[1] = u.y, q.w[2] = u.z, q.w[3] = u.w;
+    const uint2 v = *reinterpret_cast<const uint2*>(scales + r * 8);
+    q.s[0] = v.x, q.s[1] = v.y;
+  } else {
+    const uint2 u = *reinterpret_cast<const uint2*>(codes + r * 32 + m * 8);
+    q.w[0] = u.x, q.w[1] = u.y;
+    q.s[0] = *reinterpret_cast<const uint32_t*>(scales + r * 4);
+  }
+}
+// Their values as bf16, exactly, into row `key` of the operand at `base`: 128 + c
+// by masking, - 136, times the scale, two codes at a time.
+template <int D>
+__device__ __forceinline__ void store_q4_values(const Q4Words<D>& q, uint32_t base, int part, int key, int m) {
+  constexpr int NG = D / 32;
+  const __nv_bfloat162 off = __floats2bfloat162_rn(136.f, 136.f);
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    const uint32_t w = __byte_perm(q.w[g / 2], q.w[NG / 2 + g / 2], g & 1 ? 0x7632 : 0x5410);
+    const uint32_t s2 = __byte_perm(q.s[g / 2], q.s[g / 2], g & 1 ? 0x3232 : 0x1010);
+    uint32_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t c = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+      const __nv_bfloat162 x =
+          __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&c), off), *reinterpret_cast<const __nv_bfloat162*>(&s2));
+      v[i] = *reinterpret_cast<const uint32_t*>(&x);
+    }
+    const int c = 4 * g + m;
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (c / 8) * part + key * 128 +
+                                                                  (((c % 8) ^ (key & 7)) << 4)),
+                 "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
+                 : "memory");
+  }
+}
+
 template <int D>
 struct Smem {
   static constexpr int kPart = kTile * 128;           // 128 rows of 64 channels
@@ -276,6 +333,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0u;
         }
+        if constexpr (KIND == HF_CACHE_Q4) {
+          uint32_t t[8];
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) t[k] = o[e + code_place(k)];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[e + k] = t[k];
+          }
+        }
         if (live) {
           if (ns > 1) {
 #pragma unroll
@@ -323,18 +390,72 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
           const int qr = 32 * w + src;  // row in its tile
           const uint32_t dst = smem_addr(smem) + M::kQ + k * M::kOperand + (c / 8) * M::kPart + qr * 128 +
                                (((c % 8) ^ (qr & 7)) << 4);
-          cp_async_16_or_zero(dst, A.q + (a < 0 ? 0 : a * 2 + c * 16), a >= 0);
+          if constexpr (KIND == HF_CACHE_Q4) {  // channels in the order of the expanded codes
+            uint4 u = make_uint4(0, 0, 0, 0);
+            if (a >= 0) u = *reinterpret_cast<const uint4*>(A.q + a * 2 + c * 16);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(__byte_perm(u.x, u.z, 0x5410)),
+                         "r"(__byte_perm(u.x, u.z, 0x7632)), "r"(__byte_perm(u.y, u.w, 0x5410)),
+                         "r"(__byte_perm(u.y, u.w, 0x7632))
+                         : "memory");
+          } else {
+            cp_async_16_or_zero(dst, A.q + (a < 0 ? 0 : a * 2 + c * 16), a >= 0);
+          }
         }
       }
       cp_async_commit();
     }
+    const int n = 2 * n_max;
+    bool ok = true;
+    int stage = 0;
+    uint32_t phase = 1;
+    auto row_of = [&](int j) {  // of key `lane` of this warp's 32 in step j
+      const int key = (t0 + j) * kTile + 32 * w + lane;
+      return j < n_max && key < kv_end ? cache_row(C, place.seq, key) : -1;
+    };
+    if constexpr (KIND == HF_CACHE_Q4) {
+      // the words of the next operand are under way while this one is expanded
+      const char* codes[2] = {C.k + static_cast<int64_t>(h) * C.rows * (D / 2), C.v + static_cast<int64_t>(h) * C.rows * (D / 2)};
+      const char* scales[2] = {C.ks + static_cast<int64_t>(h) * C.rows * (D / 16),
+                               C.vs + static_cast<int64_t>(h) * C.rows * (D / 16)};
+      Q4Words<D> q[4];
+      const int m = lane & 3;
+      int row = row_of(0), next = row_of(1);
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
+        load_q4<D>(q[p], codes[0], scales[0], __shfl_sync(0xffffffffu, row, 8 * p + (lane >> 2)), m);
+      for (int x = 0; x < n; ++x) {
+        if (!wait_here(empty + 8 * stage, phase)) {
+          timed_out();
+          break;
+        }
+        const uint32_t base = smem_addr(smem) + M::kKV + stage * M::kOperand;
+        if (x & 1) {
+          row = next;
+          next = row_of((x >> 1) + 2);
+        }
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const int kr = 8 * p + (lane >> 2);
+          store_q4_values<D>(q[p], base, M::kPart, 32 * w + kr, m);
+          load_q4<D>(q[p], x & 1 ? codes[0] : codes[1], x & 1 ? scales[0] : scales[1],
+                     __shfl_sync(0xffffffffu, row, kr), m);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if (x == 0) mbar_arrive(qfull);
+          mbar_arrive(full + 8 * stage);
+        }
+        if (++stage == S) {
+          stage = 0;
+          phase ^= 1;
+        }
+      }
+    } else {
     const char* kb = C.k + h * C.head_stride * 2;
     const char* vb = C.v + h * C.head_stride * 2;
     constexpr int kLag = 2;
-    const int n = 2 * n_max;
-    bool ok = true;
-    int stage = 0, done = 0;
-    uint32_t phase = 1;
+    int done = 0;
     int row = -1;
     for (int x = 0; x < n + kLag && ok; ++x) {
       if (x < n) {
@@ -343,10 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
           ok = false;
           break;
         }
-        if ((x & 1) == 0) {
-          const int key = (t0 + (x >> 1)) * kTile + 32 * w + lane;
-          row = key < kv_end ? cache_row(C, place.seq, key) : -1;
-        }
+        if ((x & 1) == 0) row = row_of(x >> 1);
         const char* src = x & 1 ? vb : kb;
         const uint32_t base = smem_addr(smem) + M::kKV + stage * M::kOperand;
 #pragma unroll 4
@@ -375,9 +493,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
         if (++done == S) done = 0;
       }
     }
-    if (ok && n == 0) {
-      cp_async_wait<0>();
     }
+    cp_async_wait<0>();
   } else {
     // ------------------------------------------------------------ products
     regs_less<40>();
@@ -479,11 +596,13 @@ hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int max_kv, cuda
 }  // namespace
 
 bool attend_tiles_takes(hf_cache_kind kind, hf_dtype dtype, int D) {
-  return dtype == HF_BF16 && kind == HF_CACHE_BF16 && (D == 64 || D == 128);
+  return dtype == HF_BF16 && kind != HF_CACHE_F32 && (D == 64 || D == 128);
 }
 
 hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_kv, cudaStream_t stream) {
-  (void)kind;
+  if (kind == HF_CACHE_Q4)
+    return c.D == 64 ? launch_tiles<HF_CACHE_Q4, 64>(c, a, max_kv, stream)
+                     : launch_tiles<HF_CACHE_Q4, 128>(c, a, max_kv, stream);
   if (c.D == 64) return launch_tiles<HF_CACHE_BF16, 64>(c, a, max_kv, stream);
   return launch_tiles<HF_CACHE_BF16, 128>(c, a, max_kv, stream);
 }
