@@ -12,12 +12,18 @@
 //                   as the next product's first operand.  The running maximum
 //                   moves only when a score passes it by 2^8; the outputs in tensor
 //                   memory are rescaled then, by the same thread.
-//   warps 8-11      loaders: Q once, then K and V tiles, rows looked up page by
-//                   page, by cp.async into the 128-byte-swizzled layout; a 4-bit
-//                   cache's codes are expanded to bf16 (exactly) on the way.
-//   warp 12         issues the products: S_i = Q_i K^T from shared memory, O_i +=
-//                   P_i V with P_i in tensor memory and V as it lies (its
-//                   channels contiguous).
+//   warps 8-11      loaders, into the 128-byte-swizzled layout.  bf16: one warp
+//                   brings K and V by tensor copies, a lane a piece of a page (a
+//                   step's last rows, where the sequence ends, are cleared: what
+//                   lies there must not meet a probability of zero), the others Q;
+//                   pages that hold no multiple of eight rows come by cp.async.
+//                   4-bit: all four expand the codes to bf16 (exactly).
+//   warps 12, 13    issue the products of tile 0 and 1: S = Q K^T from shared
+//                   memory, O += P V with P in tensor memory and V as it lies
+//                   (its channels contiguous).  A warp a tile: what one spends
+//                   on its barriers lies under the other's products.  They take
+//                   turns: left to themselves both tiles fall into step, and the
+//                   softmaxes run side by side, then the products.
 // Tensor memory: S0, S1 (P over them) and O0, O1, 128 columns each.  The
 // products of one tile follow each other in issue order, so a tile's new scores
 // also say that its last product with V is done.
@@ -25,6 +31,9 @@
 // Every wait is bounded; one that runs out sets HF_CHECK_TIMEOUT and ends the
 // block.
 #include <algorithm>
+#include <string>
+
+#include <cuda.h>
 
 #include "hf_attend.cuh"
 
@@ -54,6 +63,26 @@ __device__ __forceinline__ float exp2_approx(float x) {
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Two fp32 operations an instruction.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float* a, float* b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
 
 // D[tmem] (+)= A[tmem] * B[smem]
@@ -181,8 +210,21 @@ struct Smem {
   static constexpr int kBytes = kBars + 256;
 };
 
-template <int KIND, int D>
-__global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheArgs C, const AttendArgs A, int ns) {
+// How a block gets its keys and values.
+enum Source { kByTensorCopies, kByCpAsync, kFromCodes };
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* map, int32_t x, int32_t y, int32_t z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+
+template <int SRC, int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                        const CacheArgs C, const AttendArgs A, int ns, int box) {
   using M = Smem<D>;
   constexpr int S = M::kStages;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -211,25 +253,32 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
 
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + M::kBars);
   const uint32_t full = smem_addr(bars), empty = full + 8 * S, qfull = empty + 8 * S, sfull = qfull + 8,
-                 pfull = sfull + 16, ofull = pfull + 16, drain = ofull + 16;
-  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + M::kBars + 8 * (2 * S + 8));
+                 pfull = sfull + 16, ofull = pfull + 32, turn = ofull + 16, drain = turn + 16, aux = drain + 8;
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + M::kBars + 8 * (2 * S + 13));
   if (smem_addr(smem) & 1023u) {
     if (threadIdx.x == 0) set_status(C, HF_CHECK_INTERNAL);
     return;
   }
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
-      mbar_init(full + 8 * s, 4);
-      mbar_init(empty + 8 * s, 1);
+      mbar_init(full + 8 * s, SRC == kByTensorCopies ? 1 : 4);
+      mbar_init(empty + 8 * s, 2);
     }
-    mbar_init(qfull, 4);
+    mbar_init(qfull, SRC == kByTensorCopies ? 3 : 4);
+    mbar_init(aux, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(sfull + 8 * i, 1);
-      mbar_init(pfull + 8 * i, 4);
+      mbar_init(pfull + 8 * i, 4);       // first half of the keys
+      mbar_init(pfull + 16 + 8 * i, 4);  // second half
       mbar_init(ofull + 8 * i, 1);
+      mbar_init(turn + 8 * i, 1);
     }
-    mbar_init(drain, 1);
+    mbar_init(drain, 2);
     fence_barrier_init();
+  }
+  if (SRC == kByTensorCopies && warp == 8 && lane == 0) {
+    tma_prefetch_map(&map_k);
+    tma_prefetch_map(&map_v);
   }
   if (warp == 12) {
     tmem_alloc(smem_addr(s_tmem), 512);
@@ -240,10 +289,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
   const uint32_t tmem = *s_tmem;
   auto timed_out = [&]() { set_status(C, HF_CHECK_TIMEOUT); };
 
-  // Registers, by warpgroup: 2 x 200 + 72 + 40 = 4 x 128.
+  // Registers, by warpgroup: 2 x 192 + 72 + 56 = 4 x 128.
   if (warp < 8) {
     // ------------------------------------------------------------ softmax
-    regs_more<200>();
+    regs_more<192>();
     const int i = warp >> 2;
     const int row = (warp & 3) * 32 + lane;
     const int rr = r0 + i * kTile + row;
@@ -251,6 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
     const int lim = live ? seen(span, A.causal, rr / A.G) : 0;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + i * 128 + lanes, to = tmem + 256 + i * 128 + lanes;
+    const uint64_t scale2 = pack2(A.scale_log2, A.scale_log2);
     float m = -INFINITY, l = 0.f;
     bool ok = true;
     const int n = nt[i];
@@ -272,10 +322,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
         for (int c = 0; c < 128; ++c)
           if (c >= vis) s[c] = 0xff800000u;
       }
-      float top = __uint_as_float(s[0]);
+      float top4[4];  // four chains: one would be 128 latencies long
 #pragma unroll
-      for (int c = 1; c < 128; ++c) top = fmaxf(top, __uint_as_float(s[c]));
-      top *= A.scale_log2;
+      for (int c = 0; c < 4; ++c) top4[c] = fmaxf(__uint_as_float(s[c]), __uint_as_float(s[c + 4]));
+#pragma unroll
+      for (int c = 8; c < 128; c += 8)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          top4[e] = fmaxf(top4[e], fmaxf(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 4])));
+      const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * A.scale_log2;
       if (__any_sync(0xffffffffu, top > m + kStretch)) {
         const float next = top > m + kStretch ? top : m;
         const float fix = next == m ? 1.f : exp2_approx(m - next);
@@ -293,24 +348,32 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
         }
       }
       const float base = m == -INFINITY ? 0.f : -m;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      uint64_t sum[2] = {0, 0};
 #pragma unroll
       for (int c = 0; c < 128; c += 32) {
         uint32_t p[16];
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
-          const float a = exp2_approx(fmaf(__uint_as_float(s[c + e]), A.scale_log2, base));
-          const float b = exp2_approx(fmaf(__uint_as_float(s[c + e + 1]), A.scale_log2, base));
-          sum[e / 2 % 4] += a + b;
+          float a, b;
+          unpack2(fma2(pack2(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 1])), scale2, pack2(base, base)), &a, &b);
+          a = exp2_approx(a);
+          b = exp2_approx(b);
+          sum[e / 2 % 2] = add2(sum[e / 2 % 2], pack2(a, b));
           p[e / 2] = pack_bf16(a, b);
         }
         tmem_st16(ts + c / 2, p);
+        if (c & 32) {  // 64 keys' probabilities
+          tmem_st_wait();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(pfull + (c > 64 ? 16 : 0) + 8 * i);
+        }
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      tmem_st_wait();
-      tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(pfull + 8 * i);
+      {
+        float a, b;
+        unpack2(add2(sum[0], sum[1]), &a, &b);
+        l += a + b;
+      }
     }
     // ---- outputs
     const int64_t tok = span.first + rr / A.G;
@@ -333,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0u;
         }
-        if constexpr (KIND == HF_CACHE_Q4) {
+        if constexpr (SRC == kFromCodes) {
           uint32_t t[8];
 #pragma unroll
           for (int e = 0; e < 32; e += 8) {
@@ -373,12 +436,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
     regs_less<72>();
     const int w = warp - 8;
     constexpr int kChunks = D / 8;  // 16-byte pieces of a row
-    {
-      // a lane's rows of Q: 32 (w + 4 k) + lane, k < 2
+    constexpr int kQWarps = SRC == kByTensorCopies ? 3 : 4;
+    if (SRC != kByTensorCopies || w > 0) {
 #pragma unroll 1
-      for (int k = 0; k < 2; ++k) {
+      for (int k = w + kQWarps - 4; k < 8; k += kQWarps) {  // rows 32 k ..
         int64_t at = -1;
-        const int row = 32 * (w + 4 * k) + lane;
+        const int row = 32 * k + lane;
         if (row < n_rows) {
           const int rr = r0 + row;
           at = static_cast<int64_t>(span.first + rr / A.G) * A.q_row + (h * A.G + rr % A.G) * A.q_head;
@@ -387,10 +450,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
         for (int x = 0; x < kChunks; ++x) {
           const int idx = x * 32 + lane, c = idx % kChunks, src = idx / kChunks;
           const int64_t a = __shfl_sync(0xffffffffu, at, src);
-          const int qr = 32 * w + src;  // row in its tile
-          const uint32_t dst = smem_addr(smem) + M::kQ + k * M::kOperand + (c / 8) * M::kPart + qr * 128 +
+          const int qr = 32 * (k & 3) + src;  // row in its tile
+          const uint32_t dst = smem_addr(smem) + M::kQ + (k >> 2) * M::kOperand + (c / 8) * M::kPart + qr * 128 +
                                (((c % 8) ^ (qr & 7)) << 4);
-          if constexpr (KIND == HF_CACHE_Q4) {  // channels in the order of the expanded codes
+          if constexpr (SRC == kFromCodes) {  // channels in the order of the expanded codes
             uint4 u = make_uint4(0, 0, 0, 0);
             if (a >= 0) u = *reinterpret_cast<const uint4*>(A.q + a * 2 + c * 16);
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(__byte_perm(u.x, u.z, 0x5410)),
@@ -412,7 +475,76 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
       const int key = (t0 + j) * kTile + 32 * w + lane;
       return j < n_max && key < kv_end ? cache_row(C, place.seq, key) : -1;
     };
-    if constexpr (KIND == HF_CACHE_Q4) {
+    if constexpr (SRC == kByTensorCopies) {
+      if (w > 0) {
+        cp_async_wait<0>();
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(qfull);
+      } else {
+        // Lane b + nb * c: channels 64 c .. of the rows b * box .. of a step.
+        const int nb = kTile / box, piece = lane % nb, part = lane / nb;
+        const bool active = part < D / 64;
+        auto piece_row = [&](int j) {
+          const int key = (t0 + j) * kTile + piece * box;
+          return active && j < n_max && key < kv_end ? cache_row(C, place.seq, key) : -1;
+        };
+        uint32_t aux_phase = 0;
+        int ahead = piece_row(0), issued = 0;
+        for (int j = 0; j < n_max && ok; ++j) {
+          const int row = ahead;
+          ahead = piece_row(j + 1);
+          const int key0 = (t0 + j) * kTile;
+          const unsigned there = __ballot_sync(0xffffffffu, row >= 0);
+          const bool whole = key0 + kTile <= kv_end && __popc(there) == nb * (D / 64);
+#pragma unroll 1
+          for (int v = 0; v < 2; ++v) {
+            if (!wait_here(empty + 8 * stage, phase)) {
+              timed_out();
+              ok = false;
+              break;
+            }
+            const uint32_t dst = smem_addr(smem) + M::kKV + stage * M::kOperand;
+            const uint32_t bar = whole ? full + 8 * stage : aux;
+            if (lane == 0 && there) mbar_arrive_expect_tx(bar, __popc(there) * box * 128);
+            __syncwarp();
+            ++issued;
+            if (row >= 0)
+              tma_load_3d(dst + part * M::kPart + piece * box * 128, v ? &map_v : &map_k, 64 * part, row, h, bar);
+            if (!whole) {
+              if (there) {
+                if (!wait_here(aux, aux_phase)) {
+                  timed_out();
+                  ok = false;
+                  break;
+                }
+                aux_phase ^= 1;
+              }
+              // rows past the end, and of pages that are not there: zeros
+              for (int r = lane / kChunks; r < kTile; r += 32 / kChunks) {
+                if (key0 + r >= kv_end || !(there >> (r / box) & 1)) {
+                  const int c = lane % kChunks;
+                  asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + (c / 8) * M::kPart + r * 128 +
+                                                                                (c % 8) * 16),
+                               "r"(0)
+                               : "memory");
+                }
+              }
+              fence_proxy_async_smem();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(full + 8 * stage);
+            }
+            if (++stage == S) {
+              stage = 0;
+              phase ^= 1;
+            }
+          }
+        }
+        // a block that gives up waits for its copies in flight
+        for (int x = max(issued - S, 0); !ok && x < issued; ++x)
+          if (!wait_here(full + 8 * (x % S), (x / S) & 1)) break;
+      }
+    } else if constexpr (SRC == kFromCodes) {
       // the words of the next operand are under way while this one is expanded
       const char* codes[2] = {C.k + static_cast<int64_t>(h) * C.rows * (D / 2), C.v + static_cast<int64_t>(h) * C.rows * (D / 2)};
       const char* scales[2] = {C.ks + static_cast<int64_t>(h) * C.rows * (D / 16),
@@ -481,13 +613,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
         }
       }
       cp_async_commit();
-      // what was issued kLag steps ago (before the first tile: Q) has arrived
-      cp_async_wait<kLag>();
-      if (x >= kLag) {
+      // Operands land kLag steps after they were issued; Q and the first one,
+      // which everything waits for, at once.
+      if (x == 1)
+        cp_async_wait<1>();
+      else
+        cp_async_wait<kLag>();
+      if (x == 1 || x > kLag) {
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
-          if (x == kLag) mbar_arrive(qfull);
+          if (x == 1) mbar_arrive(qfull);
           mbar_arrive(full + 8 * done);
         }
         if (++done == S) done = 0;
@@ -497,21 +633,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
     cp_async_wait<0>();
   } else {
     // ------------------------------------------------------------ products
-    regs_less<40>();
-    if (warp == 12 && lane == 0 && n_max > 0) {
+    regs_less<56>();
+    const int i = warp - 12;
+    if (i < 2 && lane == 0 && n_max > 0) {
       constexpr uint32_t idesc_s = make_idesc(1u, kTile, kTile);
       constexpr uint32_t idesc_o = make_idesc(1u, kTile, D) | (1u << 16);
       const uint32_t kv0 = smem_addr(smem) + M::kKV;
+      const uint32_t ts = tmem + i * 128, to = tmem + 256 + i * 128;
+      const uint64_t q_desc = sw128_kmajor_desc(smem_addr(smem) + M::kQ + i * M::kOperand);
+      const int n = nt[i];
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
-      auto step = [&](int* s, uint32_t* p) {  // the next stage
-        *s = stage, *p = phase;
-        if (++stage == S) {
-          stage = 0;
-          phase ^= 1;
-        }
-      };
       auto wait = [&](uint32_t bar, uint32_t parity) {
         if (ok && !wait_here(bar, parity)) {
           timed_out();
@@ -519,49 +652,67 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
         }
         return ok;
       };
-      auto scores = [&](int i, int ks) {
-        const uint64_t a = sw128_kmajor_desc(smem_addr(smem) + M::kQ + i * M::kOperand);
-        const uint64_t b = sw128_kmajor_desc(kv0 + ks * M::kOperand);
+      auto next = [&]() {
+        if (++stage == S) {
+          stage = 0;
+          phase ^= 1;
+        }
+      };
+      // A stage is released when this tile's products have read it, or, where
+      // the tile is done, at once.
+      auto release = [&](int st, bool used) {
+        if (used)
+          tc_commit(empty + 8 * st);
+        else
+          mbar_arrive(empty + 8 * st);
+      };
+      auto scores = [&](int st) {
+        const uint64_t b = sw128_kmajor_desc(kv0 + st * M::kOperand);
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
           const uint64_t off = ((c / 4) * M::kPart + (c % 4) * 32) >> 4;
-          mma_bf16(tmem + i * 128, a + off, b + off, idesc_s, c > 0);
+          mma_bf16(ts, q_desc + off, b + off, idesc_s, c > 0);
         }
         tc_commit(sfull + 8 * i);
       };
-      int ks = 0, vs = 0;
-      uint32_t kp = 0, vp = 0;
-      step(&ks, &kp);
-      if (wait(qfull, 0) && wait(full + 8 * ks, kp)) {
+      // Turns: this tile's products of step j follow the other's of step j (tile
+      // 1) or j - 1 (tile 0).
+      const uint32_t my_turn = turn + 8 * i, your_turn = turn + 8 * (1 - i);
+      if (wait(qfull, 0) && wait(full, 0) && (i == 0 || wait(my_turn, 0))) {
         tc_fence_after_sync();
-        for (int i = 0; i < 2; ++i)
-          if (nt[i] > 0) scores(i, ks);
-        tc_commit(empty + 8 * ks);
+        if (n > 0) scores(0);
+        mbar_arrive(your_turn);
+        release(0, n > 0);
       }
+      next();
       for (int j = 0; j < n_max && ok; ++j) {
-        step(&vs, &vp);
-        if (!wait(full + 8 * vs, vp)) break;
+        const int vs = stage;
+        if (!wait(full + 8 * vs, phase)) break;
+        next();
+        const int ks = stage;
         const bool more = j + 1 < n_max;
-        if (more) step(&ks, &kp);
-        for (int i = 0; i < 2 && ok; ++i) {
-          if (j < nt[i]) {
-            if (!wait(pfull + 8 * i, j & 1)) break;
-            tc_fence_after_sync();
-            const uint64_t b = sw128_mnmajor_desc(kv0 + vs * M::kOperand, M::kPart);
-#pragma unroll
-            for (int c = 0; c < kTile / 16; ++c)
-              mma_bf16_tmem_a(tmem + 256 + i * 128, tmem + i * 128 + 8 * c, b + ((c * 2048) >> 4), idesc_o,
-                              j > 0 || c > 0);
-            if (j + 1 == nt[i]) tc_commit(ofull + 8 * i);
-          }
-          if (i == 1) tc_commit(empty + 8 * vs);
-          if (more) {
-            if (i == 0 && !wait(full + 8 * ks, kp)) break;
-            if (i == 0) tc_fence_after_sync();
-            if (j + 1 < nt[i]) scores(i, ks);
-          }
+        if (more) {
+          if (!wait(full + 8 * ks, phase)) break;
+          next();
         }
-        if (more && ok) tc_commit(empty + 8 * ks);
+        if (!wait(my_turn, (j + i) & 1)) break;
+        if (j < n) {
+          const uint64_t b = sw128_mnmajor_desc(kv0 + vs * M::kOperand, M::kPart);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            if (!wait(pfull + 16 * half + 8 * i, j & 1)) break;
+            tc_fence_after_sync();
+#pragma unroll
+            for (int c = 4 * half; c < 4 * half + 4; ++c)
+              mma_bf16_tmem_a(to, ts + 8 * c, b + ((c * 2048) >> 4), idesc_o, j > 0 || c > 0);
+          }
+          if (!ok) break;
+          if (j + 1 == n) tc_commit(ofull + 8 * i);
+          if (j + 1 < n) scores(ks);
+        }
+        mbar_arrive(your_turn);
+        release(vs, j < n);
+        if (more) release(ks, j + 1 < n);
       }
       tc_commit(drain);
       if (!wait_here(drain, 0)) timed_out();
@@ -575,22 +726,76 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tiles_kernel(const CacheAr
   }
 }
 
-template <int KIND, int D>
-hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int max_kv, cudaStream_t stream) {
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    return cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+                   q == cudaDriverEntryPointSuccess
+               ? reinterpret_cast<EncodeTiledFn>(p)
+               : nullptr;
+  }();
+  return fn;
+}
+
+// Tensor map of a cache's keys or values: channels, rows, heads; boxes of `box`
+// rows of 64 channels.
+hf_status cache_map(CUtensorMap* map, const CacheArgs& c, const void* base, int box) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) {
+    set_error("cuTensorMapEncodeTiled is not available from the driver");
+    return HF_ERR_CUDA;
+  }
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(c.D), static_cast<cuuint64_t>(c.rows), static_cast<cuuint64_t>(c.H)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(c.row_stride) * 2, static_cast<cuuint64_t>(c.head_stride) * 2};
+  const cuuint32_t boxes[3] = {64, static_cast<cuuint32_t>(box), 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, boxes, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    set_error("cuTensorMapEncodeTiled failed (error " + std::to_string(static_cast<int>(r)) + ")");
+    return HF_ERR_CUDA;
+  }
+  return HF_OK;
+}
+
+template <int SRC, int D>
+hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int max_kv, int box, cudaStream_t stream) {
   const int64_t tiles = most_tiles(a.n_tok, a.G, c.n_seq, 2 * kTile) * c.H;
   // keys are split where the tiles leave SMs idle, in parts of 512 keys at least,
   // as far as the workspace goes
   int64_t ns = std::min<int64_t>(device_sm_count() / tiles, (max_kv + 511) / 512);
   ns = std::min<int64_t>(ns, part_rows(device_sm_count()) / (static_cast<int64_t>(a.n_tok) * a.H_q));
   ns = std::max<int64_t>(1, std::min<int64_t>(ns, 64));
-  auto kern = attend_tiles_kernel<KIND, D>;
+  CUtensorMap maps[2] = {};
+  if constexpr (SRC == kByTensorCopies) {
+    for (int v = 0; v < 2; ++v) {
+      const hf_status st = cache_map(&maps[v], c, v ? c.v : c.k, box);
+      if (st != HF_OK) return st;
+    }
+  }
+  auto kern = attend_tiles_kernel<SRC, D>;
   HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::kBytes),
               "hf_attend: shared memory size");
   kern<<<dim3(static_cast<unsigned>(tiles), static_cast<unsigned>(ns)), kThreads, Smem<D>::kBytes, stream>>>(
-      c, a, static_cast<int>(ns));
+      maps[0], maps[1], c, a, static_cast<int>(ns), box);
   HF_CUDA_TRY(cudaGetLastError(), "hf_attend: launch");
   if (ns > 1) return launch_join(HF_BF16, D, a, static_cast<int>(ns), stream);
   return HF_OK;
+}
+
+template <int D>
+hf_status attend_tiles_d(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_kv, cudaStream_t stream) {
+  if (kind == HF_CACHE_Q4) return launch_tiles<kFromCodes, D>(c, a, max_kv, 0, stream);
+  // rows that lie together: a page's, in pieces that divide a step
+  int box = kTile;
+  while (c.table && c.block_size % box) box /= 2;
+  if (box < 8 || c.rows == 0) return launch_tiles<kByCpAsync, D>(c, a, max_kv, 0, stream);
+  return launch_tiles<kByTensorCopies, D>(c, a, max_kv, box, stream);
 }
 
 }  // namespace
@@ -600,11 +805,7 @@ bool attend_tiles_takes(hf_cache_kind kind, hf_dtype dtype, int D) {
 }
 
 hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_kv, cudaStream_t stream) {
-  if (kind == HF_CACHE_Q4)
-    return c.D == 64 ? launch_tiles<HF_CACHE_Q4, 64>(c, a, max_kv, stream)
-                     : launch_tiles<HF_CACHE_Q4, 128>(c, a, max_kv, stream);
-  if (c.D == 64) return launch_tiles<HF_CACHE_BF16, 64>(c, a, max_kv, stream);
-  return launch_tiles<HF_CACHE_BF16, 128>(c, a, max_kv, stream);
+  return c.D == 64 ? attend_tiles_d<64>(c, a, kind, max_kv, stream) : attend_tiles_d<128>(c, a, kind, max_kv, stream);
 }
 
 }  // namespace hf
