@@ -329,7 +329,7 @@ extern "C" hf_status hf_attend(const hf_cache* cache, const hf_attend_desc* d, v
   const int64_t max_rows = static_cast<int64_t>(std::min(d->max_q_len, d->n_tok)) * a.G;
   if (attend_rows_takes(cache->kind, d->dtype, c.D) && max_rows <= 16)
     return attend_rows(c, a, cache->kind, static_cast<int>(max_rows), stream);
-  if (attend_tiles_takes(cache->kind, d->dtype, c.D)) return attend_tiles(c, a, cache->kind, max_kv, stream);
+  if (attend_tiles_takes(cache->kind, d->dtype, c.D)) return attend_tiles(c, a, cache->kind, stream);
   switch (c.D) {
     case 32: return attend_general<32>(c, a, cache->kind, d->dtype, max_kv, stream);
     case 64: return attend_general<64>(c, a, cache->kind, d->dtype, max_kv, stream);

@@ -106,7 +106,7 @@ hf_status attend_rows(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kin
 
 // The form for many query rows (hf_attend_tiles.cu): the same types and widths.
 bool attend_tiles_takes(hf_cache_kind kind, hf_dtype dtype, int D);
-hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_kv, cudaStream_t stream);
+hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, cudaStream_t stream);
 
 // Joins `ns` parts of every (token, query head), [part][token][head].
 hf_status launch_join(hf_dtype dtype, int D, const AttendArgs& a, int ns, cudaStream_t stream);

@@ -3,11 +3,15 @@
 //   S = Q K^T,  P = 2^(scale log2(e) S - m),  O += P V,  out = O / sum(P)
 //
 // Bound by the tensor cores: 4 D FLOP for every visible (query row, key) pair. A
-// block owns 256 flattened query rows of one KV head (two tiles of 128) and walks
-// its keys 128 at a time; the two tiles take turns on the tensor core, so that
-// one's softmax runs under the other's products.
+// unit is 256 flattened query rows of one KV head (two tiles of 128), whose keys
+// are walked 128 at a time; the two tiles take turns on the tensor core, so that
+// one's softmax runs under the other's products.  With at most 128 rows both tiles
+// are the same rows and take every other step.  One block an SM stays for the
+// whole call: the units' costs are shared out evenly, so long prompts end
+// together and the keys of a few short questions are split over all SMs; a
+// unit's pieces are joined by the last block at it.
 //
-//   warps 0-3, 4-7  softmax of tile 0 and 1: a thread a row.  Scores come from
+//   warps 0-3, 4-7  queries and softmax of tile 0 and 1: a thread a row.  Scores come from
 //                   tensor memory, probabilities go back there as bf16 over them,
 //                   as the next product's first operand.  The running maximum
 //                   moves only when a score passes it by 2^8; the outputs in tensor
@@ -15,8 +19,8 @@
 //   warps 8-11      loaders, into the 128-byte-swizzled layout.  bf16: one warp
 //                   brings K and V by tensor copies, a lane a piece of a page (a
 //                   step's last rows, where the sequence ends, are cleared: what
-//                   lies there must not meet a probability of zero), the others Q;
-//                   pages that hold no multiple of eight rows come by cp.async.
+//                   lies there must not meet a probability of zero); pages that
+//                   hold no multiple of eight rows come by cp.async.
 //                   4-bit: all four expand the codes to bf16 (exactly).
 //   warps 12, 13    issue the products of tile 0 and 1: S = Q K^T from shared
 //                   memory, O += P V with P in tensor memory and V as it lies
@@ -24,6 +28,7 @@
 //                   on its barriers lies under the other's products.  They take
 //                   turns: left to themselves both tiles fall into step, and the
 //                   softmaxes run side by side, then the products.
+//   warp 14         works out the next piece of the block's share.
 // Tensor memory: S0, S1 (P over them) and O0, O1, 128 columns each.  The
 // products of one tile follow each other in issue order, so a tile's new scores
 // also say that its last product with V is done.
@@ -85,16 +90,63 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return r;
 }
 
-// D[tmem] (+)= A[tmem] * B[smem]
-__device__ __forceinline__ void mma_bf16_tmem_a(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
-                                                uint32_t accumulate) {
+#define HF_R4(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3])
+#define HF_W4(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3])
+
+// A whole sector a lane, 32-byte aligned.
+__device__ __forceinline__ void store_32_bytes(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), HF_W4(w, 0), HF_W4(w, 4) : "memory");
+}
+
+// Products are issued by whole warps, one lane's by predicate: a branch on a lane
+// would keep addresses and descriptors out of the uniform registers that the
+// instruction takes them from, and moving them there costs more than a product
+// takes where other warps want the issue slots (16 products beside eight busy
+// warps: 1,570 cycles by a branch, 1,027 by predicate).
+__device__ __forceinline__ uint32_t elected_lane() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r;
+}
+// D[tmem] (+)= A[smem] * B[smem]
+__device__ __forceinline__ void mma_if(uint32_t on, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                       uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(on)
       : "memory");
 }
+// D[tmem] (+)= A[tmem] * B[smem]
+__device__ __forceinline__ void mma_tmem_a_if(uint32_t on, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc,
+                                              uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(on)
+      : "memory");
+}
+__device__ __forceinline__ void commit_if(uint32_t on, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+      "r"(on)
+      : "memory");
+}
+__device__ __forceinline__ void arrive_if(uint32_t on, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t.reg .b64 st;\n\t"
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "@q mbarrier.arrive.shared::cta.b64 st, [%0];\n\t}" ::"r"(bar),
+      "r"(on)
+      : "memory");
+}
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 // Descriptor of an operand whose rows (K) are 128-byte pieces of the other
 // dimension, 128-byte swizzle: 1,024 bytes from eight rows of K to the next
@@ -116,8 +168,6 @@ __device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity) {
   }
 }
 
-#define HF_R4(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3])
-#define HF_W4(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3])
 // 32 columns of this thread's lane.
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
   asm volatile(
@@ -199,17 +249,6 @@ __device__ __forceinline__ void store_q4_values(const Q4Words<D>& q, uint32_t ba
   }
 }
 
-template <int D>
-struct Smem {
-  static constexpr int kPart = kTile * 128;           // 128 rows of 64 channels
-  static constexpr int kOperand = kPart * (D / 64);   // a tile of Q, K or V
-  static constexpr int kStages = D == 128 ? 5 : 6;
-  static constexpr int kQ = 0;
-  static constexpr int kKV = 2 * kOperand;
-  static constexpr int kBars = kKV + kStages * kOperand;
-  static constexpr int kBytes = kBars + 256;
-};
-
 // How a block gets its keys and values.
 enum Source { kByTensorCopies, kByCpAsync, kFromCodes };
 
@@ -221,59 +260,110 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* map, int32
       : "memory");
 }
 
+// ---------------------------------------------------------------------------
+// Who does what
+// ---------------------------------------------------------------------------
+// A unit is 256 query rows of one KV head, its cost about its keys: visible keys
+// times G, plus 256 G (what starting and ending one takes, two steps of 128
+// keys).  Within a head the costs grow linearly with the unit (causal), so sums
+// of them have a closed form.  All units' costs, laid end to end, are shared out
+// evenly over the blocks; a share's ends fall inside units, which are cut there
+// at whole steps.
+constexpr int kMaxBlocks = 160;  // bits of Piece::mask
+
+struct Piece {
+  int32_t valid;
+  int32_t seq, first, n, kv;     // SeqSpan
+  int32_t h, r0, n_rows;
+  int32_t t0, n_ops;             // key steps t0 .. t0 + n_ops - 1
+  int32_t nt[2];                 // steps of tile 0 and 1
+  int32_t kv_end;
+  int32_t dual;                  // at most 128 rows: both tiles are the same rows, and take the steps in turn
+  int32_t n_pieces;              // of the unit, in blocks c0 .. c1
+  int32_t c0, c1;
+  int32_t slot, slot0;           // of this piece, and of block c0's
+  uint32_t mask[kMaxBlocks / 32];  // blocks c0 + i that have one
+};
+
+struct UnitCost {
+  int64_t w0, dw, head;  // cost of unit 0, its growth, all units of one head
+  int tiles;
+};
+__device__ __forceinline__ UnitCost unit_cost(const SeqSpan& s, const AttendArgs& A) {
+  UnitCost u;
+  const int64_t rows = static_cast<int64_t>(s.n) * A.G;
+  u.tiles = static_cast<int>((rows + 2 * kTile - 1) / (2 * kTile));
+  u.dw = A.causal ? 2 * kTile : 0;
+  u.w0 = (A.causal ? max(s.kv - s.n, 0) : s.kv) * static_cast<int64_t>(A.G) + u.dw + 2 * kTile * A.G;
+  u.head = u.tiles * u.w0 + u.dw * (static_cast<int64_t>(u.tiles) * (u.tiles - 1) / 2);
+  return u;
+}
+
+// Cuts of a unit with cost [w0, w0 + w) and n steps: the step where cost x lies.
+// A piece of less than two steps goes to its neighbour.
+__device__ __forceinline__ int cut(int64_t x, int64_t w0, int64_t w, int n) {
+  if (x <= w0) return 0;
+  if (x >= w0 + w) return n;
+  const int p = static_cast<int>(static_cast<double>(x - w0) / static_cast<double>(w) * n);
+  return p < 2 ? 0 : p > n - 2 ? n : p;
+}
+
+template <int SRC, int D>
+struct Smem {
+  static constexpr int kPart = kTile * 128;           // 128 rows of 64 channels
+  static constexpr int kOperand = kPart * (D / 64);   // a tile of Q, K or V
+  static constexpr int kStages = D == 128 ? 5 : 6;
+  static constexpr int kQ = 0;
+  static constexpr int kKV = 2 * kOperand;
+  static constexpr int kRest = kKV + kStages * kOperand;
+  static constexpr int kLoaders = SRC == kByTensorCopies ? 1 : 4;
+  static constexpr int kReaders = 8 + (SRC == kByTensorCopies ? 2 : 4) + 2;  // warps that read a piece
+};
+// What follows the operands in shared memory.
+template <int S>
+struct Shared {
+  uint64_t full[S], empty[S], tail[S];
+  uint64_t q_full[2], s_full[2], p_full[2][2], o_full[2], turn[2];
+  uint64_t piece_full[2], piece_empty[2];
+  uint64_t drain, aux, meet;
+  float2 ml[2 * kTile];
+  Piece piece[2];
+  uint32_t tmem;
+  int32_t last;
+};
+
 template <int SRC, int D>
 __global__ void __launch_bounds__(kThreads, 1)
     attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                        const CacheArgs C, const AttendArgs A, int ns, int box) {
-  using M = Smem<D>;
+                        const CacheArgs C, const AttendArgs A, int box) {
+  using M = Smem<SRC, D>;
   constexpr int S = M::kStages;
   extern __shared__ __align__(1024) uint8_t smem[];
+  Shared<S>& sh = *reinterpret_cast<Shared<S>*>(smem + M::kRest);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-
-  // ---- the block's rows and keys
-  const int h = blockIdx.x % C.H, sp = blockIdx.y;
-  const TilePlace place = find_tile(C, A, 2 * kTile, blockIdx.x / C.H);
-  if (place.seq >= C.n_seq) return;
-  const SeqSpan span = seq_span(C, A, place.seq);
-  const int r0 = (place.tiles - 1 - place.at) * 2 * kTile;  // the longest first
-  const int n_rows = static_cast<int>(min(static_cast<int64_t>(2 * kTile), static_cast<int64_t>(span.n) * A.G - r0));
-  // keys of this part: tiles [t0, t1) of 128; of query tile i: up to its last row's
-  const int kv_end = seen(span, A.causal, (r0 + n_rows - 1) / A.G);
-  const int all = (kv_end + kTile - 1) / kTile;
-  const int t0 = static_cast<int>(static_cast<int64_t>(all) * sp / ns);
-  const int t1 = static_cast<int>(static_cast<int64_t>(all) * (sp + 1) / ns);
-  int nt[2];
-  {
-    const int last0 = min(n_rows, kTile) - 1;
-    const int end0 = seen(span, A.causal, (r0 + last0) / A.G);
-    nt[0] = max(min((end0 + kTile - 1) / kTile, t1) - t0, 0);
-    nt[1] = n_rows > kTile ? t1 - t0 : 0;
-  }
-  const int n_max = max(nt[0], nt[1]);
-
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + M::kBars);
-  const uint32_t full = smem_addr(bars), empty = full + 8 * S, qfull = empty + 8 * S, sfull = qfull + 8,
-                 pfull = sfull + 16, ofull = pfull + 32, turn = ofull + 16, drain = turn + 16, aux = drain + 8;
-  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + M::kBars + 8 * (2 * S + 13));
   if (smem_addr(smem) & 1023u) {
     if (threadIdx.x == 0) set_status(C, HF_CHECK_INTERNAL);
     return;
   }
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
-      mbar_init(full + 8 * s, SRC == kByTensorCopies ? 1 : 4);
-      mbar_init(empty + 8 * s, 2);
+      mbar_init(smem_addr(&sh.full[s]), M::kLoaders);
+      mbar_init(smem_addr(&sh.empty[s]), 2);
+      mbar_init(smem_addr(&sh.tail[s]), 1);
     }
-    mbar_init(qfull, SRC == kByTensorCopies ? 3 : 4);
-    mbar_init(aux, 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(sfull + 8 * i, 1);
-      mbar_init(pfull + 8 * i, 4);       // first half of the keys
-      mbar_init(pfull + 16 + 8 * i, 4);  // second half
-      mbar_init(ofull + 8 * i, 1);
-      mbar_init(turn + 8 * i, 1);
+      mbar_init(smem_addr(&sh.q_full[i]), 4);
+      mbar_init(smem_addr(&sh.s_full[i]), 1);
+      mbar_init(smem_addr(&sh.p_full[0][i]), 4);  // first 64 keys
+      mbar_init(smem_addr(&sh.p_full[1][i]), 4);  // the others
+      mbar_init(smem_addr(&sh.o_full[i]), 1);
+      mbar_init(smem_addr(&sh.turn[i]), 1);
+      mbar_init(smem_addr(&sh.piece_full[i]), 1);
+      mbar_init(smem_addr(&sh.piece_empty[i]), M::kReaders);
     }
-    mbar_init(drain, 2);
+    mbar_init(smem_addr(&sh.drain), 2);
+    mbar_init(smem_addr(&sh.aux), 1);
+    mbar_init(smem_addr(&sh.meet), 8);
     fence_barrier_init();
   }
   if (SRC == kByTensorCopies && warp == 8 && lane == 0) {
@@ -281,13 +371,32 @@ __global__ void __launch_bounds__(kThreads, 1)
     tma_prefetch_map(&map_v);
   }
   if (warp == 12) {
-    tmem_alloc(smem_addr(s_tmem), 512);
+    tmem_alloc(smem_addr(&sh.tmem), 512);
     tmem_relinquish();
   }
   __syncthreads();
   tc_fence_after_sync();
-  const uint32_t tmem = *s_tmem;
-  auto timed_out = [&]() { set_status(C, HF_CHECK_TIMEOUT); };
+  const uint32_t tmem = sh.tmem;
+  bool ok = true;  // this warp's waits so far
+  // By one thread; by a whole warp, whose lanes go on or give up together.
+  auto wait_one = [&](const uint64_t& bar, uint32_t parity) {
+    if (ok && !wait_here(smem_addr(&bar), parity)) {
+      set_status(C, HF_CHECK_TIMEOUT);
+      ok = false;
+    }
+    return ok;
+  };
+  auto wait = [&](const uint64_t& bar, uint32_t parity) {
+    wait_one(bar, parity);
+    return ok = __all_sync(0xffffffffu, ok);
+  };
+  // Piece k, once it is there; released by the warp's lane 0.
+  auto piece_at = [&](int k) -> const Piece& { return sh.piece[k & 1]; };
+  auto piece_wait = [&](int k) { return wait(sh.piece_full[k & 1], (k >> 1) & 1); };
+  auto piece_done = [&](int k) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_addr(&sh.piece_empty[k & 1]));
+  };
 
   // Registers, by warpgroup: 2 x 192 + 72 + 56 = 4 x 128.
   if (warp < 8) {
@@ -295,363 +404,484 @@ __global__ void __launch_bounds__(kThreads, 1)
     regs_more<192>();
     const int i = warp >> 2;
     const int row = (warp & 3) * 32 + lane;
-    const int rr = r0 + i * kTile + row;
-    const bool live = i * kTile + row < n_rows;
-    const int lim = live ? seen(span, A.causal, rr / A.G) : 0;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + i * 128 + lanes, to = tmem + 256 + i * 128 + lanes;
+    const bool sectors = ((reinterpret_cast<uintptr_t>(A.out) | (A.o_row * 2) | (A.o_head * 2)) & 31) == 0;
     const uint64_t scale2 = pack2(A.scale_log2, A.scale_log2);
-    float m = -INFINITY, l = 0.f;
-    bool ok = true;
-    const int n = nt[i];
-    for (int j = 0; j < n; ++j) {
-      if (!wait_here(sfull + 8 * i, j & 1)) {
-        timed_out();
-        ok = false;
-        break;
+    // This warp's 32 rows of a piece's queries, into shared memory.
+    auto load_q = [&](const Piece& pc) {
+      constexpr int kChunks = D / 8;  // 16-byte pieces of a row
+      const int r = row + (pc.dual ? 0 : i * kTile);
+      int64_t at = -1;
+      if (r < pc.n_rows) {
+        const int rr = pc.r0 + r;
+        at = static_cast<int64_t>(pc.first + rr / A.G) * A.q_row + (pc.h * A.G + rr % A.G) * A.q_head;
       }
-      tc_fence_after_sync();
-      uint32_t s[128];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32(ts + 32 * c, s + 32 * c);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld_wait32(s + 32 * c);
-      const int vis = lim - (t0 + j) * kTile;  // columns that this row sees
-      if (__any_sync(0xffffffffu, vis < kTile)) {
-#pragma unroll
-        for (int c = 0; c < 128; ++c)
-          if (c >= vis) s[c] = 0xff800000u;
+#pragma unroll 4
+      for (int x = 0; x < kChunks; ++x) {
+        const int idx = x * 32 + lane, c = idx % kChunks, src = idx / kChunks;
+        const int64_t a = __shfl_sync(0xffffffffu, at, src);
+        const int qr = (warp & 3) * 32 + src;  // row in its tile
+        const uint32_t dst = smem_addr(smem) + M::kQ + i * M::kOperand + (c / 8) * M::kPart + qr * 128 +
+                             (((c % 8) ^ (qr & 7)) << 4);
+        if constexpr (SRC == kFromCodes) {  // channels in the order of the expanded codes
+          uint4 u = make_uint4(0, 0, 0, 0);
+          if (a >= 0) u = *reinterpret_cast<const uint4*>(A.q + a * 2 + c * 16);
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(__byte_perm(u.x, u.z, 0x5410)),
+                       "r"(__byte_perm(u.x, u.z, 0x7632)), "r"(__byte_perm(u.y, u.w, 0x5410)),
+                       "r"(__byte_perm(u.y, u.w, 0x7632))
+                       : "memory");
+        } else {
+          cp_async_16_or_zero(dst, A.q + (a < 0 ? 0 : a * 2 + c * 16), a >= 0);
+        }
       }
-      float top4[4];  // four chains: one would be 128 latencies long
+      cp_async_commit();
+    };
+    auto q_there = [&]() {
+      cp_async_wait<0>();
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[i]));
+    };
+    // All eight warps of both tiles, like a barrier but bounded.
+    uint32_t meet_phase = 0;
+    auto meet = [&]() {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_addr(&sh.meet));
+      wait(sh.meet, meet_phase);
+      meet_phase ^= 1;
+      return ok;
+    };
+    uint32_t s_phase = 0, o_phase = 0;
+    // Only of pieces in which this tile takes part: the products' warp waits for
+    // those alone, so that it is never a phase behind.
+    if (piece_wait(0) && piece_at(0).valid && piece_at(0).nt[i] > 0) {
+      load_q(piece_at(0));
+      q_there();
+    }
+    for (int k = 0; ok && piece_at(k).valid; ++k) {
+      const Piece& pc = piece_at(k);
+      const int dual = pc.dual, n = pc.nt[i], r0 = pc.r0, n_rows = pc.n_rows;
+      const SeqSpan span = {pc.first, pc.n, pc.kv};
+      const int r = row + (dual ? 0 : i * kTile);
+      const bool live = r < n_rows;
+      const int token = (r0 + r) / A.G, head = r0 + r - token * A.G;
+      const int lim = live ? seen(span, A.causal, token) : 0;
+      int key0 = (pc.t0 + (dual ? i : 0)) * kTile;
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < n; ++j, key0 += dual ? 2 * kTile : kTile) {
+        if (!wait(sh.s_full[i], s_phase)) break;
+        s_phase ^= 1;
+        tc_fence_after_sync();
+        uint32_t s[128];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) top4[c] = fmaxf(__uint_as_float(s[c]), __uint_as_float(s[c + 4]));
+        for (int c = 0; c < 4; ++c) tmem_ld32(ts + 32 * c, s + 32 * c);
 #pragma unroll
-      for (int c = 8; c < 128; c += 8)
+        for (int c = 0; c < 4; ++c) tmem_ld_wait32(s + 32 * c);
+        const int vis = lim - key0;  // columns that this row sees
+        if (__any_sync(0xffffffffu, vis < kTile)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          top4[e] = fmaxf(top4[e], fmaxf(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 4])));
-      const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * A.scale_log2;
-      if (__any_sync(0xffffffffu, top > m + kStretch)) {
-        const float next = top > m + kStretch ? top : m;
-        const float fix = next == m ? 1.f : exp2_approx(m - next);
-        m = next;
-        l *= fix;
-        if (j > 0) {
+          for (int c = 0; c < 128; ++c)
+            if (c >= vis) s[c] = 0xff800000u;
+        }
+        float top4[4];  // four chains: one would be 128 latencies long
 #pragma unroll
-          for (int c = 0; c < D; c += 16) {
-            uint32_t o[16];
-            tmem_load_16(to + c, o);
+        for (int c = 0; c < 4; ++c) top4[c] = fmaxf(__uint_as_float(s[c]), __uint_as_float(s[c + 4]));
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fix);
-            tmem_st16(to + c, o);
+        for (int c = 8; c < 128; c += 8)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            top4[e] = fmaxf(top4[e], fmaxf(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 4])));
+        const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * A.scale_log2;
+        if (__any_sync(0xffffffffu, top > m + kStretch)) {
+          const float next = top > m + kStretch ? top : m;
+          const float fix = next == m ? 1.f : exp2_approx(m - next);
+          m = next;
+          l *= fix;
+          if (j > 0) {
+#pragma unroll
+            for (int c = 0; c < D; c += 16) {
+              uint32_t o[16];
+              tmem_load_16(to + c, o);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fix);
+              tmem_st16(to + c, o);
+            }
           }
         }
-      }
-      const float base = m == -INFINITY ? 0.f : -m;
-      uint64_t sum[2] = {0, 0};
+        const float base = m == -INFINITY ? 0.f : -m;
+        uint64_t sum[2] = {0, 0};
 #pragma unroll
-      for (int c = 0; c < 128; c += 32) {
-        uint32_t p[16];
+        for (int c = 0; c < 128; c += 32) {
+          uint32_t p[16];
 #pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-          float a, b;
-          unpack2(fma2(pack2(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 1])), scale2, pack2(base, base)), &a, &b);
-          a = exp2_approx(a);
-          b = exp2_approx(b);
-          sum[e / 2 % 2] = add2(sum[e / 2 % 2], pack2(a, b));
-          p[e / 2] = pack_bf16(a, b);
+          for (int e = 0; e < 32; e += 2) {
+            float a, b;
+            unpack2(fma2(pack2(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 1])), scale2, pack2(base, base)), &a,
+                    &b);
+            a = exp2_approx(a);
+            b = exp2_approx(b);
+            sum[e / 2 % 2] = add2(sum[e / 2 % 2], pack2(a, b));
+            p[e / 2] = pack_bf16(a, b);
+          }
+          tmem_st16(ts + c / 2, p);
+          if (c & 32) {  // 64 keys' probabilities
+            tmem_st_wait();
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&sh.p_full[c > 64][i]));
+          }
         }
-        tmem_st16(ts + c / 2, p);
-        if (c & 32) {  // 64 keys' probabilities
-          tmem_st_wait();
-          tc_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(pfull + (c > 64 ? 16 : 0) + 8 * i);
-        }
-      }
-      {
         float a, b;
         unpack2(add2(sum[0], sum[1]), &a, &b);
         l += a + b;
       }
-    }
-    // ---- outputs
-    const int64_t tok = span.first + rr / A.G;
-    const int hq = h * A.G + rr % A.G;
-    if (ok && n > 0 && !wait_here(ofull + 8 * i, 0)) {
-      timed_out();
-      ok = false;
-    }
-    if (ok) {
-      tc_fence_after_sync();
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const int64_t slot = (static_cast<int64_t>(sp) * A.n_tok + tok) * A.H_q + hq;
-#pragma unroll
-      for (int c = 0; c < D; c += 32) {
-        uint32_t o[32];
-        if (n > 0) {
-          tmem_ld32(to + c, o);
-          tmem_ld_wait32(o);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0u;
+      // The next piece's queries: this tile's last scores are there, so nothing
+      // reads the present ones.
+      const bool more = piece_wait(k + 1) && piece_at(k + 1).valid;
+      const bool more_q = more && piece_at(k + 1).nt[i] > 0;
+      if (more_q) load_q(piece_at(k + 1));
+      // ---- outputs
+      if (n > 0) {
+        if (!wait(sh.o_full[i], o_phase)) break;
+        o_phase ^= 1;
+        tc_fence_after_sync();
+      }
+      if (!ok) break;
+      if (dual) {
+        // the same rows: tile 1's outputs go into tile 0's
+        if (i == 1) {
+          sh.ml[row] = make_float2(m, l);
+          tc_fence_before_sync();
         }
-        if constexpr (SRC == kFromCodes) {
-          uint32_t t[8];
+        if (!meet()) break;
+        if (i == 0 && pc.nt[1] > 0) {
+          tc_fence_after_sync();
+          const float2 ml = sh.ml[row];
+          const float next = fmaxf(m, ml.x), zero = next == -INFINITY ? 0.f : next;
+          const float mine = exp2_approx(m - zero), other = exp2_approx(ml.x - zero);
+          m = next;
+          l = l * mine + ml.y * other;
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
+          for (int c = 0; c < D; c += 16) {
+            uint32_t o[16], o1[16];
+            tmem_load_16(to + c, o);
+            tmem_load_16(to + 128 + c, o1);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) t[k] = o[e + code_place(k)];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) o[e + k] = t[k];
+            for (int e = 0; e < 16; ++e)
+              o[e] = __float_as_uint(__uint_as_float(o[e]) * mine + __uint_as_float(o1[e]) * other);
+            tmem_st16(to + c, o);
           }
+          tmem_st_wait();
         }
-        if (live) {
-          if (ns > 1) {
+      }
+      const bool writes = live && !(dual && i == 1);
+      if (!(dual && i == 1)) {
+        const bool whole = pc.n_pieces == 1;
+        const int64_t tok = span.first + token;
+        const int hq = pc.h * A.G + head;
+        const int64_t at = static_cast<int64_t>(pc.slot) * (2 * kTile) + r;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<uint4*>(A.part_o + slot * D + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          if (n > 0) {
+            tmem_ld32(to + c, o);
+            tmem_ld_wait32(o);
           } else {
-            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(A.out) + tok * A.o_row + hq * A.o_head + c;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = 0u;
+          }
+          if constexpr (SRC == kFromCodes) {
+            uint32_t t[8];
 #pragma unroll
             for (int e = 0; e < 32; e += 8) {
-              uint32_t w[4];
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                w[k] = pack_bf16(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
-              *reinterpret_cast<uint4*>(dst + e) = make_uint4(w[0], w[1], w[2], w[3]);
+              for (int x = 0; x < 8; ++x) t[x] = o[e + code_place(x)];
+#pragma unroll
+              for (int x = 0; x < 8; ++x) o[e + x] = t[x];
+            }
+          }
+          if (writes && !whole) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) store_32_bytes(A.part_o + at * D + c + e, o + e);
+          } else if (writes) {
+            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(A.out) + tok * A.o_row + hq * A.o_head + c;
+            uint32_t w[16];
+#pragma unroll
+            for (int x = 0; x < 16; ++x)
+              w[x] = pack_bf16(__uint_as_float(o[2 * x]) * inv, __uint_as_float(o[2 * x + 1]) * inv);
+            if (sectors) {
+              store_32_bytes(dst, w);
+              store_32_bytes(dst + 16, w + 8);
+            } else {
+#pragma unroll
+              for (int x = 0; x < 4; ++x)
+                reinterpret_cast<uint4*>(dst)[x] = make_uint4(w[4 * x], w[4 * x + 1], w[4 * x + 2], w[4 * x + 3]);
             }
           }
         }
-      }
-      if (live) {
-        if (ns > 1)
-          A.part_ml[slot] = make_float2(m, l);
-        else if (A.lse)
+        if (writes && !whole)
+          A.part_ml[at] = make_float2(m, l);
+        else if (writes && A.lse)
           A.lse[tok * A.H_q + hq] = (m + log2f(l)) * 0.693147180559945309f;
       }
+      if (dual) {  // tile 1's outputs have been read
+        tc_fence_before_sync();
+        if (!meet()) break;
+        tc_fence_after_sync();
+      }
+      if (more_q) q_there();
+      if (pc.n_pieces > 1) {
+        // the last block at the unit joins its pieces, in the blocks' order
+        __threadfence();
+        if (!meet()) break;
+        if (threadIdx.x == 0) {
+          sh.last = atomicAdd(A.zeroed + pc.c0, 1) == pc.n_pieces - 1;
+          if (sh.last) A.zeroed[pc.c0] = 0;
+          __threadfence();
+        }
+        if (!meet()) break;
+        if (sh.last) {
+          const int blocks = pc.c1 - pc.c0 + 1;
+          auto has = [&](int b) { return pc.mask[b >> 5] >> (b & 31) & 1; };
+          auto row_at = [&](int b) { return static_cast<int64_t>(b ? 2 * (pc.c0 + b) : pc.slot0) * (2 * kTile); };
+          if (static_cast<int>(threadIdx.x) < n_rows) {  // a row's maximum and sum
+            const int q = threadIdx.x;
+            float top = -INFINITY;
+#pragma unroll 4
+            for (int b = 0; b < blocks; ++b)
+              if (has(b)) top = fmaxf(top, __ldcg(&A.part_ml[row_at(b) + q]).x);
+            const float zero = top == -INFINITY ? 0.f : top;
+            float sum = 0.f;
+#pragma unroll 4
+            for (int b = 0; b < blocks; ++b) {
+              if (!has(b)) continue;
+              const float2 ml = __ldcg(&A.part_ml[row_at(b) + q]);
+              sum = fmaf(ml.y, exp2_approx(ml.x - zero), sum);
+            }
+            sh.ml[q] = make_float2(zero, sum == 0.f ? 0.f : 1.f / sum);
+            if (A.lse) {
+              const int rr = r0 + q;
+              A.lse[(span.first + rr / A.G) * static_cast<int64_t>(A.H_q) + pc.h * A.G + rr % A.G] =
+                  (top + log2f(sum)) * 0.693147180559945309f;
+            }
+          }
+          if (!meet()) break;
+          constexpr int kAt = 8;  // elements of a thread on the way at once
+          for (int x0 = threadIdx.x; x0 < n_rows * (D / 4); x0 += 256 * kAt) {
+            float4 acc[kAt];
+#pragma unroll
+            for (int e = 0; e < kAt; ++e) acc[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int b = 0; b < blocks; ++b) {
+              if (!has(b)) continue;
+              float4 v[kAt];
+              float f[kAt];
+#pragma unroll
+              for (int e = 0; e < kAt; ++e) {
+                const int x = min(x0 + 256 * e, n_rows * (D / 4) - 1);
+                const int64_t at = row_at(b) + x / (D / 4);
+                v[e] = __ldcg(reinterpret_cast<const float4*>(A.part_o + at * D + x % (D / 4) * 4));
+                f[e] = __ldcg(&A.part_ml[at]).x;
+              }
+#pragma unroll
+              for (int e = 0; e < kAt; ++e) {
+                const int x = min(x0 + 256 * e, n_rows * (D / 4) - 1);
+                const float2 zi = sh.ml[x / (D / 4)];
+                const float g = exp2_approx(f[e] - zi.x) * zi.y;
+                acc[e].x = fmaf(v[e].x, g, acc[e].x);
+                acc[e].y = fmaf(v[e].y, g, acc[e].y);
+                acc[e].z = fmaf(v[e].z, g, acc[e].z);
+                acc[e].w = fmaf(v[e].w, g, acc[e].w);
+              }
+            }
+#pragma unroll
+            for (int e = 0; e < kAt; ++e) {
+              const int x = x0 + 256 * e;
+              if (x < n_rows * (D / 4)) {
+                const int rr = r0 + x / (D / 4);
+                __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(A.out) +
+                                     (span.first + rr / A.G) * A.o_row + (pc.h * A.G + rr % A.G) * A.o_head + x % (D / 4) * 4;
+                *reinterpret_cast<uint2*>(dst) =
+                    make_uint2(pack_bf16(acc[e].x, acc[e].y), pack_bf16(acc[e].z, acc[e].w));
+              }
+            }
+          }
+        }
+        if (!meet()) break;  // sh.last is read
+      }
+      piece_done(k);
+      if (!more) break;
     }
   } else if (warp < 12) {
     // ------------------------------------------------------------ loaders
     regs_less<72>();
     const int w = warp - 8;
     constexpr int kChunks = D / 8;  // 16-byte pieces of a row
-    constexpr int kQWarps = SRC == kByTensorCopies ? 3 : 4;
-    if (SRC != kByTensorCopies || w > 0) {
-#pragma unroll 1
-      for (int k = w + kQWarps - 4; k < 8; k += kQWarps) {  // rows 32 k ..
-        int64_t at = -1;
-        const int row = 32 * k + lane;
-        if (row < n_rows) {
-          const int rr = r0 + row;
-          at = static_cast<int64_t>(span.first + rr / A.G) * A.q_row + (h * A.G + rr % A.G) * A.q_head;
-        }
-#pragma unroll 4
-        for (int x = 0; x < kChunks; ++x) {
-          const int idx = x * 32 + lane, c = idx % kChunks, src = idx / kChunks;
-          const int64_t a = __shfl_sync(0xffffffffu, at, src);
-          const int qr = 32 * (k & 3) + src;  // row in its tile
-          const uint32_t dst = smem_addr(smem) + M::kQ + (k >> 2) * M::kOperand + (c / 8) * M::kPart + qr * 128 +
-                               (((c % 8) ^ (qr & 7)) << 4);
-          if constexpr (SRC == kFromCodes) {  // channels in the order of the expanded codes
-            uint4 u = make_uint4(0, 0, 0, 0);
-            if (a >= 0) u = *reinterpret_cast<const uint4*>(A.q + a * 2 + c * 16);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(__byte_perm(u.x, u.z, 0x5410)),
-                         "r"(__byte_perm(u.x, u.z, 0x7632)), "r"(__byte_perm(u.y, u.w, 0x5410)),
-                         "r"(__byte_perm(u.y, u.w, 0x7632))
-                         : "memory");
-          } else {
-            cp_async_16_or_zero(dst, A.q + (a < 0 ? 0 : a * 2 + c * 16), a >= 0);
-          }
-        }
-      }
-      cp_async_commit();
-    }
-    const int n = 2 * n_max;
-    bool ok = true;
+    auto clear_row = [&](uint32_t operand, int r, int c) {
+      asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(operand + (c / 8) * M::kPart + r * 128 + (c % 8) * 16),
+                   "r"(0)
+                   : "memory");
+    };
     int stage = 0;
     uint32_t phase = 1;
-    auto row_of = [&](int j) {  // of key `lane` of this warp's 32 in step j
-      const int key = (t0 + j) * kTile + 32 * w + lane;
-      return j < n_max && key < kv_end ? cache_row(C, place.seq, key) : -1;
+    auto next = [&]() {
+      if (++stage == S) {
+        stage = 0;
+        phase ^= 1;
+      }
     };
-    if constexpr (SRC == kByTensorCopies) {
-      if (w > 0) {
-        cp_async_wait<0>();
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(qfull);
-      } else {
-        // Lane b + nb * c: channels 64 c .. of the rows b * box .. of a step.
-        const int nb = kTile / box, piece = lane % nb, part = lane / nb;
-        const bool active = part < D / 64;
-        auto piece_row = [&](int j) {
-          const int key = (t0 + j) * kTile + piece * box;
-          return active && j < n_max && key < kv_end ? cache_row(C, place.seq, key) : -1;
+    if (w < M::kLoaders) {
+      uint32_t aux_phase = 0;
+      int issued = 0;
+      for (int k = 0; piece_wait(k) && piece_at(k).valid; ++k) {
+        const int seq = piece_at(k).seq, h = piece_at(k).h, t0 = piece_at(k).t0, n_ops = piece_at(k).n_ops,
+                  kv_end = piece_at(k).kv_end;
+        piece_done(k);
+        auto row_of = [&](int j, int key) {  // of key `key` of step j
+          key += (t0 + j) * kTile;
+          return j < n_ops && key < kv_end ? cache_row(C, seq, key) : -1;
         };
-        uint32_t aux_phase = 0;
-        int ahead = piece_row(0), issued = 0;
-        for (int j = 0; j < n_max && ok; ++j) {
-          const int row = ahead;
-          ahead = piece_row(j + 1);
-          const int key0 = (t0 + j) * kTile;
-          const unsigned there = __ballot_sync(0xffffffffu, row >= 0);
-          const bool whole = key0 + kTile <= kv_end && __popc(there) == nb * (D / 64);
+        if constexpr (SRC == kByTensorCopies) {
+          // Lane b + nb * c: channels 64 c .. of the rows b * box .. of a step.
+          const int nb = kTile / box, piece = lane % nb, part = lane / nb;
+          const bool active = part < D / 64;
+          int ahead = active ? row_of(0, piece * box) : -1;
+          for (int j = 0; j < n_ops && ok; ++j) {
+            const int row = ahead;
+            ahead = active ? row_of(j + 1, piece * box) : -1;
+            const int key0 = (t0 + j) * kTile;
+            const unsigned there = __ballot_sync(0xffffffffu, row >= 0);
+            const bool bad = there != __ballot_sync(0xffffffffu, active && key0 + piece * box < kv_end);
+            const bool ends = key0 + kTile > kv_end;
 #pragma unroll 1
-          for (int v = 0; v < 2; ++v) {
-            if (!wait_here(empty + 8 * stage, phase)) {
-              timed_out();
-              ok = false;
-              break;
+            for (int v = 0; v < 2; ++v) {
+              if (!wait(sh.empty[stage], phase)) break;
+              const uint32_t dst = smem_addr(smem) + M::kKV + stage * M::kOperand;
+              const uint32_t bar = smem_addr(bad ? &sh.aux : v && ends ? &sh.tail[stage] : &sh.full[stage]);
+              if (lane == 0 && there) mbar_arrive_expect_tx(bar, __popc(there) * box * 128);
+              __syncwarp();
+              ++issued;
+              if (row >= 0)
+                tma_load_3d(dst + part * M::kPart + piece * box * 128, v ? &map_v : &map_k, 64 * part, row, h, bar);
+              if (bad) {  // rows of pages that are not there: zeros
+                if (there) {
+                  if (!wait(sh.aux, aux_phase)) break;
+                  aux_phase ^= 1;
+                }
+                for (int r = lane / kChunks; r < kTile; r += 32 / kChunks)
+                  if (!(there >> (r / box) & 1)) clear_row(dst, r, lane % kChunks);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(v && ends ? &sh.tail[stage] : &sh.full[stage]));
+              }
+              next();
             }
-            const uint32_t dst = smem_addr(smem) + M::kKV + stage * M::kOperand;
-            const uint32_t bar = whole ? full + 8 * stage : aux;
-            if (lane == 0 && there) mbar_arrive_expect_tx(bar, __popc(there) * box * 128);
+          }
+        } else if constexpr (SRC == kFromCodes) {
+          // the words of the next operand are under way while this one is expanded
+          const char* codes[2] = {C.k + static_cast<int64_t>(h) * C.rows * (D / 2),
+                                  C.v + static_cast<int64_t>(h) * C.rows * (D / 2)};
+          const char* scales[2] = {C.ks + static_cast<int64_t>(h) * C.rows * (D / 16),
+                                   C.vs + static_cast<int64_t>(h) * C.rows * (D / 16)};
+          Q4Words<D> q[4];
+          const int m = lane & 3;
+          int row = row_of(0, 32 * w + lane), later = row_of(1, 32 * w + lane);
+#pragma unroll
+          for (int p = 0; p < 4; ++p)
+            load_q4<D>(q[p], codes[0], scales[0], __shfl_sync(0xffffffffu, row, 8 * p + (lane >> 2)), m);
+          for (int x = 0; x < 2 * n_ops; ++x) {
+            if (!wait(sh.empty[stage], phase)) break;
+            const uint32_t base = smem_addr(smem) + M::kKV + stage * M::kOperand;
+            if (x & 1) {
+              row = later;
+              later = row_of((x >> 1) + 2, 32 * w + lane);
+            }
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+              const int kr = 8 * p + (lane >> 2);
+              store_q4_values<D>(q[p], base, M::kPart, 32 * w + kr, m);
+              load_q4<D>(q[p], x & 1 ? codes[0] : codes[1], x & 1 ? scales[0] : scales[1],
+                         __shfl_sync(0xffffffffu, row, kr), m);
+            }
+            fence_proxy_async_smem();
             __syncwarp();
-            ++issued;
-            if (row >= 0)
-              tma_load_3d(dst + part * M::kPart + piece * box * 128, v ? &map_v : &map_k, 64 * part, row, h, bar);
-            if (!whole) {
-              if (there) {
-                if (!wait_here(aux, aux_phase)) {
-                  timed_out();
-                  ok = false;
-                  break;
-                }
-                aux_phase ^= 1;
+            if (lane == 0) mbar_arrive(smem_addr(&sh.full[stage]));
+            next();
+          }
+        } else {
+          const char* kb = C.k + h * C.head_stride * 2;
+          const char* vb = C.v + h * C.head_stride * 2;
+          int row = -1, done = stage;
+          for (int x = 0; x <= 2 * n_ops; ++x) {
+            if (x < 2 * n_ops) {
+              if (!wait(sh.empty[stage], phase)) break;
+              if ((x & 1) == 0) row = row_of(x >> 1, 32 * w + lane);
+              const char* src = x & 1 ? vb : kb;
+              const uint32_t base = smem_addr(smem) + M::kKV + stage * M::kOperand;
+#pragma unroll 4
+              for (int y = 0; y < kChunks; ++y) {
+                const int idx = y * 32 + lane, c = idx % kChunks, kr = idx / kChunks;
+                const int r = __shfl_sync(0xffffffffu, row, kr);
+                const int key = 32 * w + kr;
+                cp_async_16_or_zero(base + (c / 8) * M::kPart + key * 128 + (((c % 8) ^ (key & 7)) << 4),
+                                    src + max(r, 0) * (C.row_stride * 2) + c * 16, r >= 0);
               }
-              // rows past the end, and of pages that are not there: zeros
-              for (int r = lane / kChunks; r < kTile; r += 32 / kChunks) {
-                if (key0 + r >= kv_end || !(there >> (r / box) & 1)) {
-                  const int c = lane % kChunks;
-                  asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + (c / 8) * M::kPart + r * 128 +
-                                                                                (c % 8) * 16),
-                               "r"(0)
-                               : "memory");
-                }
-              }
+              next();
+            }
+            cp_async_commit();
+            cp_async_wait<1>();  // the operand before this one has landed
+            if (x > 0) {
               fence_proxy_async_smem();
               __syncwarp();
-              if (lane == 0) mbar_arrive(full + 8 * stage);
-            }
-            if (++stage == S) {
-              stage = 0;
-              phase ^= 1;
+              if (lane == 0) mbar_arrive(smem_addr(&sh.full[done]));
+              if (++done == S) done = 0;
             }
           }
         }
-        // a block that gives up waits for its copies in flight
+        if (!ok) break;
+      }
+      cp_async_wait<0>();
+      // a block that gives up waits for its copies in flight
+      if (SRC == kByTensorCopies)
         for (int x = max(issued - S, 0); !ok && x < issued; ++x)
-          if (!wait_here(full + 8 * (x % S), (x / S) & 1)) break;
-      }
-    } else if constexpr (SRC == kFromCodes) {
-      // the words of the next operand are under way while this one is expanded
-      const char* codes[2] = {C.k + static_cast<int64_t>(h) * C.rows * (D / 2), C.v + static_cast<int64_t>(h) * C.rows * (D / 2)};
-      const char* scales[2] = {C.ks + static_cast<int64_t>(h) * C.rows * (D / 16),
-                               C.vs + static_cast<int64_t>(h) * C.rows * (D / 16)};
-      Q4Words<D> q[4];
-      const int m = lane & 3;
-      int row = row_of(0), next = row_of(1);
-#pragma unroll
-      for (int p = 0; p < 4; ++p)
-        load_q4<D>(q[p], codes[0], scales[0], __shfl_sync(0xffffffffu, row, 8 * p + (lane >> 2)), m);
-      for (int x = 0; x < n; ++x) {
-        if (!wait_here(empty + 8 * stage, phase)) {
-          timed_out();
-          break;
-        }
-        const uint32_t base = smem_addr(smem) + M::kKV + stage * M::kOperand;
-        if (x & 1) {
-          row = next;
-          next = row_of((x >> 1) + 2);
-        }
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          const int kr = 8 * p + (lane >> 2);
-          store_q4_values<D>(q[p], base, M::kPart, 32 * w + kr, m);
-          load_q4<D>(q[p], x & 1 ? codes[0] : codes[1], x & 1 ? scales[0] : scales[1],
-                     __shfl_sync(0xffffffffu, row, kr), m);
-        }
+          if (!wait_here(smem_addr(&sh.full[x % S]), (x / S) & 1)) break;
+    } else if (SRC == kByTensorCopies && w == 1) {
+      // Where a sequence ends inside a step, the rows of V behind its end that a
+      // product still reads (16 keys at a time) are cleared once they are there.
+      uint32_t tail_phase = 0;  // a bit a stage
+      int ops = 0;
+      for (int k = 0; piece_wait(k) && piece_at(k).valid; ++k) {
+        const int t0 = piece_at(k).t0, n_ops = piece_at(k).n_ops, kv_end = piece_at(k).kv_end;
+        piece_done(k);
+        ops += 2 * n_ops;
+        const int from = kv_end - (t0 + n_ops - 1) * kTile;
+        if (n_ops == 0 || from >= kTile) continue;
+        const int st = (ops - 1) % S;
+        if (!wait(sh.tail[st], tail_phase >> st & 1)) break;
+        tail_phase ^= 1u << st;
+        for (int r = from + lane / kChunks; r < ((from + 15) & ~15); r += 32 / kChunks)
+          clear_row(smem_addr(smem) + M::kKV + st * M::kOperand, r, lane % kChunks);
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) {
-          if (x == 0) mbar_arrive(qfull);
-          mbar_arrive(full + 8 * stage);
-        }
-        if (++stage == S) {
-          stage = 0;
-          phase ^= 1;
-        }
-      }
-    } else {
-    const char* kb = C.k + h * C.head_stride * 2;
-    const char* vb = C.v + h * C.head_stride * 2;
-    constexpr int kLag = 2;
-    int done = 0;
-    int row = -1;
-    for (int x = 0; x < n + kLag && ok; ++x) {
-      if (x < n) {
-        if (!wait_here(empty + 8 * stage, phase)) {
-          timed_out();
-          ok = false;
-          break;
-        }
-        if ((x & 1) == 0) row = row_of(x >> 1);
-        const char* src = x & 1 ? vb : kb;
-        const uint32_t base = smem_addr(smem) + M::kKV + stage * M::kOperand;
-#pragma unroll 4
-        for (int y = 0; y < kChunks; ++y) {
-          const int idx = y * 32 + lane, c = idx % kChunks, kr = idx / kChunks;
-          const int r = __shfl_sync(0xffffffffu, row, kr);
-          const int key = 32 * w + kr;
-          cp_async_16_or_zero(base + (c / 8) * M::kPart + key * 128 + (((c % 8) ^ (key & 7)) << 4),
-                              src + max(r, 0) * (C.row_stride * 2) + c * 16, r >= 0);
-        }
-        if (++stage == S) {
-          stage = 0;
-          phase ^= 1;
-        }
-      }
-      cp_async_commit();
-      // Operands land kLag steps after they were issued; Q and the first one,
-      // which everything waits for, at once.
-      if (x == 1)
-        cp_async_wait<1>();
-      else
-        cp_async_wait<kLag>();
-      if (x == 1 || x > kLag) {
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-          if (x == 1) mbar_arrive(qfull);
-          mbar_arrive(full + 8 * done);
-        }
-        if (++done == S) done = 0;
+        if (lane == 0) mbar_arrive(smem_addr(&sh.full[st]));
       }
     }
-    }
-    cp_async_wait<0>();
   } else {
-    // ------------------------------------------------------------ products
     regs_less<56>();
-    const int i = warp - 12;
-    if (i < 2 && lane == 0 && n_max > 0) {
+    const int i = uniform(warp - 12);
+    if (i < 2) {
+      // ---------------------------------------------------------- products
       constexpr uint32_t idesc_s = make_idesc(1u, kTile, kTile);
       constexpr uint32_t idesc_o = make_idesc(1u, kTile, D) | (1u << 16);
+      const uint32_t on = elected_lane();
+      const uint32_t tm = static_cast<uint32_t>(uniform(static_cast<int>(tmem)));
       const uint32_t kv0 = smem_addr(smem) + M::kKV;
-      const uint32_t ts = tmem + i * 128, to = tmem + 256 + i * 128;
+      const uint32_t ts = tm + i * 128, to = tm + 256 + i * 128;
       const uint64_t q_desc = sw128_kmajor_desc(smem_addr(smem) + M::kQ + i * M::kOperand);
-      const int n = nt[i];
       int stage = 0;
-      uint32_t phase = 0;
-      bool ok = true;
-      auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok && !wait_here(bar, parity)) {
-          timed_out();
-          ok = false;
-        }
-        return ok;
-      };
+      uint32_t phase = 0, p_phase = 0, q_phase = 0;
+      uint32_t batch = 0;
       auto next = [&]() {
         if (++stage == S) {
           stage = 0;
@@ -659,65 +889,202 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       };
       // A stage is released when this tile's products have read it, or, where
-      // the tile is done, at once.
+      // it takes no part, at once.
       auto release = [&](int st, bool used) {
         if (used)
-          tc_commit(empty + 8 * st);
+          commit_if(on, smem_addr(&sh.empty[st]));
         else
-          mbar_arrive(empty + 8 * st);
+          arrive_if(on, smem_addr(&sh.empty[st]));
       };
       auto scores = [&](int st) {
         const uint64_t b = sw128_kmajor_desc(kv0 + st * M::kOperand);
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
           const uint64_t off = ((c / 4) * M::kPart + (c % 4) * 32) >> 4;
-          mma_bf16(ts, q_desc + off, b + off, idesc_s, c > 0);
+          mma_if(on, ts, q_desc + off, b + off, idesc_s, c > 0);
         }
-        tc_commit(sfull + 8 * i);
+        commit_if(on, smem_addr(&sh.s_full[i]));
       };
-      // Turns: this tile's products of step j follow the other's of step j (tile
-      // 1) or j - 1 (tile 0).
-      const uint32_t my_turn = turn + 8 * i, your_turn = turn + 8 * (1 - i);
-      if (wait(qfull, 0) && wait(full, 0) && (i == 0 || wait(my_turn, 0))) {
+      // Turns: batch b of this tile's products follows batch b (tile 1) or b - 1
+      // (tile 0) of the other's.
+      auto turn_wait = [&]() { return i == 0 && batch == 0 ? ok : wait(sh.turn[i], (batch + i + 1) & 1); };
+      auto turn_pass = [&]() {
+        ++batch;
+        arrive_if(on, smem_addr(&sh.turn[1 - i]));
+      };
+      for (int k = 0; piece_wait(k) && uniform(piece_at(k).valid); ++k) {
+        const int n_ops = uniform(piece_at(k).n_ops), n = uniform(piece_at(k).nt[i]);
+        const bool dual = uniform(piece_at(k).dual);
+        const int keys = uniform(piece_at(k).kv_end - piece_at(k).t0 * kTile);
+        piece_done(k);
+        if (n > 0) {
+          if (!wait(sh.q_full[i], q_phase)) break;
+          q_phase ^= 1;
+        }
+        if (n_ops == 0) continue;
+        auto mine = [&](int o) { return dual ? (o & 1) == i : o < n; };
+        const int last = dual ? 2 * (n - 1) + i : n - 1;
+        uint32_t accumulate = 0;
+        if (!wait(sh.full[stage], phase) || !(dual || turn_wait())) break;
         tc_fence_after_sync();
-        if (n > 0) scores(0);
-        mbar_arrive(your_turn);
-        release(0, n > 0);
-      }
-      next();
-      for (int j = 0; j < n_max && ok; ++j) {
-        const int vs = stage;
-        if (!wait(full + 8 * vs, phase)) break;
+        if (mine(0)) scores(stage);
+        if (!dual) turn_pass();
+        release(stage, mine(0));
         next();
-        const int ks = stage;
-        const bool more = j + 1 < n_max;
-        if (more) {
-          if (!wait(full + 8 * ks, phase)) break;
+        for (int o = 0; o < n_ops; ++o) {
+          const int vs = stage;
+          if (!wait(sh.full[vs], phase)) break;
           next();
-        }
-        if (!wait(my_turn, (j + i) & 1)) break;
-        if (j < n) {
-          const uint64_t b = sw128_mnmajor_desc(kv0 + vs * M::kOperand, M::kPart);
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            if (!wait(pfull + 16 * half + 8 * i, j & 1)) break;
-            tc_fence_after_sync();
-#pragma unroll
-            for (int c = 4 * half; c < 4 * half + 4; ++c)
-              mma_bf16_tmem_a(to, ts + 8 * c, b + ((c * 2048) >> 4), idesc_o, j > 0 || c > 0);
+          const int ks = stage;
+          const bool more = o + 1 < n_ops;
+          if (more) {
+            if (!wait(sh.full[ks], phase)) break;
+            next();
           }
-          if (!ok) break;
-          if (j + 1 == n) tc_commit(ofull + 8 * i);
-          if (j + 1 < n) scores(ks);
+          if (!dual && !turn_wait()) break;
+          tc_fence_after_sync();
+          if (mine(o)) {
+            const uint64_t b = sw128_mnmajor_desc(kv0 + vs * M::kOperand, M::kPart);
+            // 16 keys a product; behind the sequence's end there is nothing to add
+            const int groups = (min(keys - o * kTile, kTile) + 15) / 16;
+            if (!wait(sh.p_full[0][i], p_phase)) break;
+            tc_fence_after_sync();
+            if (groups == kTile / 16) {
+#pragma unroll
+              for (int c = 0; c < 4; ++c)
+                mma_tmem_a_if(on, to, ts + 8 * c, b + ((c * 2048) >> 4), idesc_o, c ? 1u : accumulate);
+              if (!wait(sh.p_full[1][i], p_phase)) break;
+              tc_fence_after_sync();
+#pragma unroll
+              for (int c = 4; c < 8; ++c) mma_tmem_a_if(on, to, ts + 8 * c, b + ((c * 2048) >> 4), idesc_o, 1u);
+            } else {
+              if (!wait(sh.p_full[1][i], p_phase)) break;
+              tc_fence_after_sync();
+              for (int c = 0; c < groups; ++c)
+                mma_tmem_a_if(on, to, ts + 8 * c, b + ((c * 2048) >> 4), idesc_o, c ? 1u : accumulate);
+            }
+            p_phase ^= 1;
+            accumulate = 1;
+            if (o == last) commit_if(on, smem_addr(&sh.o_full[i]));
+          }
+          const bool then = more && mine(o + 1);
+          if (then) scores(ks);
+          if (!dual) turn_pass();
+          release(vs, mine(o));
+          if (more) release(ks, then);
         }
-        mbar_arrive(your_turn);
-        release(vs, j < n);
-        if (more) release(ks, j + 1 < n);
+        if (!ok) break;
       }
-      tc_commit(drain);
-      if (!wait_here(drain, 0)) timed_out();
+      commit_if(on, smem_addr(&sh.drain));
+      if (!wait_here(smem_addr(&sh.drain), 0)) set_status(C, HF_CHECK_TIMEOUT);
+      __syncwarp();
+    } else if (i == 2) {
+      // ---------------------------------------------------------- what comes next
+      int64_t total = 0;
+      for (int s = lane; s < C.n_seq; s += 32) total += C.H * unit_cost(seq_span(C, A, s), A).head;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      // shares of four steps at least
+      const int64_t n_cta = max(min(static_cast<int64_t>(gridDim.x), total / (4 * kTile * A.G)), static_cast<int64_t>(1));
+      const int64_t cta = blockIdx.x;
+      auto begin = [&](int64_t c) { return c * total / n_cta; };
+      int64_t x = cta < n_cta ? begin(cta) : total;
+      const int64_t x0 = x, x1 = cta < n_cta ? begin(cta + 1) : total;
+      int k = 0;
+      int64_t base = 0;  // cost before sequence group `group`
+      int group = 0;
+      while (ok) {
+        Piece pc;
+        pc.valid = 0;
+        while (x < x1) {
+          // the sequence of cost x
+          int64_t before = 0;
+          int seq = 0;
+          for (;; group += 32) {
+            const int s = group + lane;
+            const int64_t mine = s < C.n_seq ? C.H * unit_cost(seq_span(C, A, s), A).head : 0;
+            int64_t sum = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+              const int64_t v = __shfl_up_sync(0xffffffffu, sum, o);
+              if (lane >= o) sum += v;
+            }
+            const unsigned past = __ballot_sync(0xffffffffu, base + sum > x);
+            if (past || group + 32 >= C.n_seq) {
+              const int l = past ? __ffs(past) - 1 : 31;
+              seq = group + l;
+              before = base + __shfl_sync(0xffffffffu, sum - mine, l);
+              break;
+            }
+            base += __shfl_sync(0xffffffffu, sum, 31);
+          }
+          if (seq >= C.n_seq) {
+            x = x1;
+            break;
+          }
+          const SeqSpan span = seq_span(C, A, seq);
+          const UnitCost u = unit_cost(span, A);
+          auto upto = [&](int64_t at) { return at * u.w0 + u.dw * (at * (at - 1) / 2); };
+          const int h = static_cast<int>((x - before) / u.head);
+          const int64_t in_head = x - before - h * u.head;
+          int lo = 0, hi = u.tiles - 1;
+          while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (upto(mid) <= in_head)
+              lo = mid;
+            else
+              hi = mid - 1;
+          }
+          const int64_t w0 = before + h * u.head + upto(lo), w = u.w0 + u.dw * lo, w1 = w0 + w;
+          pc.seq = seq, pc.first = span.first, pc.n = span.n, pc.kv = span.kv;
+          pc.h = h;
+          pc.r0 = lo * 2 * kTile;
+          pc.n_rows = static_cast<int>(min(static_cast<int64_t>(2 * kTile), static_cast<int64_t>(span.n) * A.G - pc.r0));
+          pc.kv_end = seen(span, A.causal, (pc.r0 + pc.n_rows - 1) / A.G);
+          const int all = (pc.kv_end + kTile - 1) / kTile, steps = max(all, 1);
+          const int p0 = cut(x, w0, w, steps), p1 = cut(min(x1, w1), w0, w, steps);
+          if (p0 < p1) {
+            pc.valid = 1;
+            pc.t0 = p0;
+            const int t1 = min(p1, all);
+            pc.dual = pc.n_rows <= kTile;
+            const int n = max(t1 - p0, 0);
+            if (pc.dual) {
+              pc.nt[0] = (n + 1) / 2;
+              pc.nt[1] = n / 2;
+              pc.n_ops = n;
+            } else {
+              const int end0 = (seen(span, A.causal, (pc.r0 + kTile - 1) / A.G) + kTile - 1) / kTile;
+              pc.nt[0] = max(min(end0, t1) - p0, 0);
+              pc.nt[1] = n;
+              pc.n_ops = n;
+            }
+            pc.c0 = static_cast<int>(((w0 + 1) * n_cta - 1) / total);
+            pc.c1 = static_cast<int>((w1 * n_cta - 1) / total);
+            pc.slot0 = 2 * pc.c0 + (begin(pc.c0) == w0 ? 0 : 1);
+            pc.slot = static_cast<int>(2 * cta) + (x == x0 ? 0 : 1);
+            pc.n_pieces = 0;
+#pragma unroll
+            for (int b = 0; b < kMaxBlocks; b += 32) {
+              const int64_t c = pc.c0 + b + lane;
+              const bool has = c <= pc.c1 && cut(max(begin(c), w0), w0, w, steps) < cut(min(begin(c + 1), w1), w0, w, steps);
+              pc.mask[b / 32] = __ballot_sync(0xffffffffu, has);
+              pc.n_pieces += __popc(pc.mask[b / 32]);
+            }
+          }
+          x = w1;
+          if (pc.valid) break;
+        }
+        if (k > 1 && !wait(sh.piece_empty[k & 1], ((k >> 1) + 1) & 1)) break;
+        if (lane == 0) {
+          sh.piece[k & 1] = pc;
+          mbar_arrive(smem_addr(&sh.piece_full[k & 1]));
+        }
+        __syncwarp();
+        ++k;
+        if (!pc.valid) break;
+      }
     }
-    __syncwarp();
   }
   __syncthreads();
   if (warp == 12) {
@@ -764,13 +1131,7 @@ hf_status cache_map(CUtensorMap* map, const CacheArgs& c, const void* base, int 
 }
 
 template <int SRC, int D>
-hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int max_kv, int box, cudaStream_t stream) {
-  const int64_t tiles = most_tiles(a.n_tok, a.G, c.n_seq, 2 * kTile) * c.H;
-  // keys are split where the tiles leave SMs idle, in parts of 512 keys at least,
-  // as far as the workspace goes
-  int64_t ns = std::min<int64_t>(device_sm_count() / tiles, (max_kv + 511) / 512);
-  ns = std::min<int64_t>(ns, part_rows(device_sm_count()) / (static_cast<int64_t>(a.n_tok) * a.H_q));
-  ns = std::max<int64_t>(1, std::min<int64_t>(ns, 64));
+hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int box, cudaStream_t stream) {
   CUtensorMap maps[2] = {};
   if constexpr (SRC == kByTensorCopies) {
     for (int v = 0; v < 2; ++v) {
@@ -779,23 +1140,22 @@ hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int max_kv, int 
     }
   }
   auto kern = attend_tiles_kernel<SRC, D>;
-  HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::kBytes),
+  constexpr int kBytes = Smem<SRC, D>::kRest + static_cast<int>(sizeof(Shared<Smem<SRC, D>::kStages>));
+  HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes),
               "hf_attend: shared memory size");
-  kern<<<dim3(static_cast<unsigned>(tiles), static_cast<unsigned>(ns)), kThreads, Smem<D>::kBytes, stream>>>(
-      maps[0], maps[1], c, a, static_cast<int>(ns), box);
+  kern<<<std::min(device_sm_count(), kMaxBlocks), kThreads, kBytes, stream>>>(maps[0], maps[1], c, a, box);
   HF_CUDA_TRY(cudaGetLastError(), "hf_attend: launch");
-  if (ns > 1) return launch_join(HF_BF16, D, a, static_cast<int>(ns), stream);
   return HF_OK;
 }
 
 template <int D>
-hf_status attend_tiles_d(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_kv, cudaStream_t stream) {
-  if (kind == HF_CACHE_Q4) return launch_tiles<kFromCodes, D>(c, a, max_kv, 0, stream);
+hf_status attend_tiles_d(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, cudaStream_t stream) {
+  if (kind == HF_CACHE_Q4) return launch_tiles<kFromCodes, D>(c, a, 0, stream);
   // rows that lie together: a page's, in pieces that divide a step
   int box = kTile;
   while (c.table && c.block_size % box) box /= 2;
-  if (box < 8 || c.rows == 0) return launch_tiles<kByCpAsync, D>(c, a, max_kv, 0, stream);
-  return launch_tiles<kByTensorCopies, D>(c, a, max_kv, box, stream);
+  if (box < 8 || c.rows == 0) return launch_tiles<kByCpAsync, D>(c, a, 0, stream);
+  return launch_tiles<kByTensorCopies, D>(c, a, box, stream);
 }
 
 }  // namespace
@@ -804,8 +1164,8 @@ bool attend_tiles_takes(hf_cache_kind kind, hf_dtype dtype, int D) {
   return dtype == HF_BF16 && kind != HF_CACHE_F32 && (D == 64 || D == 128);
 }
 
-hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_kv, cudaStream_t stream) {
-  return c.D == 64 ? attend_tiles_d<64>(c, a, kind, max_kv, stream) : attend_tiles_d<128>(c, a, kind, max_kv, stream);
+hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, cudaStream_t stream) {
+  return c.D == 64 ? attend_tiles_d<64>(c, a, kind, stream) : attend_tiles_d<128>(c, a, kind, stream);
 }
 
 }  // namespace hf
