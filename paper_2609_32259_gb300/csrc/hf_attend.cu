@@ -65,6 +65,8 @@ __global__ void __launch_bounds__(kThreads) attend_general_kernel(const CacheArg
   float* sV = sK + kKeys * (D + 4);
   float* sP = sV + kKeys * D;
   int* sRow = reinterpret_cast<int*>(sP + kRows * (kKeys + 1));
+  depend_wait();
+  depend_launch();
   const TilePlace at = find_tile(C, A, kRows, blockIdx.x);
   if (at.seq >= C.n_seq) return;
   const SeqSpan span = seq_span(C, A, at.seq);
@@ -183,6 +185,8 @@ __global__ void __launch_bounds__(kThreads) attend_general_kernel(const CacheArg
 // A warp joins the parts of one (token, query head).
 template <typename T, int D>
 __global__ void __launch_bounds__(128) attend_join_kernel(const AttendArgs A, int ns) {
+  depend_wait();
+  depend_launch();
   const int64_t row = blockIdx.x * static_cast<int64_t>(4) + (threadIdx.x >> 5);
   const int64_t n = static_cast<int64_t>(A.n_tok) * A.H_q;
   if (row >= n) return;
@@ -222,9 +226,9 @@ hf_status launch_general(const CacheArgs& c, const AttendArgs& a, int max_kv, cu
   HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                    static_cast<int>(general_smem<D>())),
               "hf_attend: shared memory size");
-  kern<<<dim3(static_cast<unsigned>(tiles), c.H, static_cast<unsigned>(ns)), kThreads, general_smem<D>(), stream>>>(
-      c, a, static_cast<int>(ns));
-  HF_CUDA_TRY(cudaGetLastError(), "hf_attend: launch");
+  HF_CUDA_TRY(launch_dependent(kern, dim3(static_cast<unsigned>(tiles), c.H, static_cast<unsigned>(ns)), dim3(kThreads),
+                               general_smem<D>(), stream, c, a, static_cast<int>(ns)),
+              "hf_attend: launch");
   if (ns > 1) return launch_join(sizeof(T) == 2 ? HF_BF16 : HF_F32, D, a, static_cast<int>(ns), stream);
   return HF_OK;
 }
@@ -232,11 +236,9 @@ hf_status launch_general(const CacheArgs& c, const AttendArgs& a, int max_kv, cu
 template <int D>
 hf_status launch_join_d(hf_dtype dtype, const AttendArgs& a, int ns, cudaStream_t stream) {
   const unsigned blocks = static_cast<unsigned>((static_cast<int64_t>(a.n_tok) * a.H_q + 3) / 4);
-  if (dtype == HF_BF16)
-    attend_join_kernel<__nv_bfloat16, D><<<blocks, 128, 0, stream>>>(a, ns);
-  else
-    attend_join_kernel<float, D><<<blocks, 128, 0, stream>>>(a, ns);
-  HF_CUDA_TRY(cudaGetLastError(), "hf_attend: joining launch");
+  HF_CUDA_TRY(launch_dependent(dtype == HF_BF16 ? attend_join_kernel<__nv_bfloat16, D> : attend_join_kernel<float, D>,
+                               dim3(blocks), dim3(128), 0, stream, a, ns),
+              "hf_attend: joining launch");
   return HF_OK;
 }
 

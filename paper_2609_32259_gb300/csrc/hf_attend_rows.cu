@@ -144,6 +144,8 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
   uint8_t* ring = smem + warp * R::kWarpBytes;
   const uint32_t ring_a = smem_addr(ring);
 
+  depend_wait();
+  depend_launch();
   // Steps of the sequences before each one.
   {
     int64_t carry = 0;
@@ -597,8 +599,8 @@ hf_status launch_rows(const CacheArgs& c, const AttendArgs& a, cudaStream_t stre
   constexpr int smem = Ring<KIND, D>::kWarpBytes * kWarps;
   HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem),
               "hf_attend: shared memory size");
-  kern<<<device_sm_count() * kBlocks<KIND, NT>, kThreads, smem, stream>>>(c, a);
-  HF_CUDA_TRY(cudaGetLastError(), "hf_attend: launch");
+  HF_CUDA_TRY(launch_dependent(kern, dim3(device_sm_count() * kBlocks<KIND, NT>), dim3(kThreads), smem, stream, c, a),
+              "hf_attend: launch");
   return HF_OK;
 }
 

@@ -70,6 +70,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 // Two fp32 operations an instruction.
 __device__ __forceinline__ uint64_t pack2(float a, float b) {
   uint64_t r;
@@ -269,7 +274,7 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* map, int32
 // of them have a closed form.  All units' costs, laid end to end, are shared out
 // evenly over the blocks; a share's ends fall inside units, which are cut there
 // at whole steps.
-constexpr int kMaxBlocks = 160;  // bits of Piece::mask
+constexpr int kMaxBlocks = 160;  // bits of a mask of blocks
 
 struct Piece {
   int32_t valid;
@@ -279,10 +284,10 @@ struct Piece {
   int32_t nt[2];                 // steps of tile 0 and 1
   int32_t kv_end;
   int32_t dual;                  // at most 128 rows: both tiles are the same rows, and take the steps in turn
+  // complete when the next piece is announced:
   int32_t n_pieces;              // of the unit, in blocks c0 .. c1
   int32_t c0, c1;
   int32_t slot, slot0;           // of this piece, and of block c0's
-  uint32_t mask[kMaxBlocks / 32];  // blocks c0 + i that have one
 };
 
 struct UnitCost {
@@ -304,8 +309,21 @@ __device__ __forceinline__ UnitCost unit_cost(const SeqSpan& s, const AttendArgs
 __device__ __forceinline__ int cut(int64_t x, int64_t w0, int64_t w, int n) {
   if (x <= w0) return 0;
   if (x >= w0 + w) return n;
-  const int p = static_cast<int>(static_cast<double>(x - w0) / static_cast<double>(w) * n);
+  // fp32, rounded the same way by every block: it has to grow with x and no more
+  const int p = static_cast<int>(static_cast<float>(x - w0) / static_cast<float>(w) * n);
   return p < 2 ? 0 : p > n - 2 ? n : p;
+}
+// floor(x / d), x >= 0, d > 0: fp32 quotients, put right (a 64-bit division is
+// some hundred instructions).
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t d) {
+  int64_t q = 0, r = x;
+  const float inv = 1.f / static_cast<float>(d);
+  while (r < 0 || r >= d) {
+    const int64_t step = static_cast<int64_t>(static_cast<float>(r) * inv);
+    q += step != 0 ? step : r < 0 ? -1 : 1;
+    r = x - q * d;
+  }
+  return q;
 }
 
 template <int SRC, int D>
@@ -328,6 +346,7 @@ struct Shared {
   uint64_t drain, aux, meet;
   float2 ml[2 * kTile];
   Piece piece[2];
+  uint32_t mask[2][kMaxBlocks / 32];  // blocks c0 + i that have a piece of its unit
   uint32_t tmem;
   int32_t last;
 };
@@ -374,6 +393,28 @@ __global__ void __launch_bounds__(kThreads, 1)
     tmem_alloc(smem_addr(&sh.tmem), 512);
     tmem_relinquish();
   }
+  // Warp 14: a lane a sequence, its cost and the sum up to it.
+  int group = 0;
+  SeqSpan group_span = {};
+  int64_t group_cost = 0, group_sum = 0;
+  auto load_group = [&](int g) {
+    group = g;
+    group_cost = 0;
+    if (g + lane < C.n_seq) {
+      group_span = seq_span(C, A, g + lane);
+      group_cost = C.H * unit_cost(group_span, A).head;
+    }
+    group_sum = group_cost;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, group_sum, o);
+      if (lane >= o) group_sum += v;
+    }
+  };
+  // What the kernel before this one writes is read from here on.
+  depend_wait();
+  depend_launch();
+  if (warp == 14) load_group(0);
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = sh.tmem;
@@ -490,8 +531,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int c = 8; c < 128; c += 8)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            top4[e] = fmaxf(top4[e], fmaxf(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 4])));
+          for (int e = 0; e < 4; ++e) top4[e] = max3(top4[e], __uint_as_float(s[c + e]), __uint_as_float(s[c + e + 4]));
         const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * A.scale_log2;
         if (__any_sync(0xffffffffu, top > m + kStretch)) {
           const float next = top > m + kStretch ? top : m;
@@ -548,6 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_after_sync();
       }
       if (!ok) break;
+      if (more_q) q_there();  // its first scores come while the outputs go
       if (dual) {
         // the same rows: tile 1's outputs go into tile 0's
         if (i == 1) {
@@ -631,7 +672,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!meet()) break;
         tc_fence_after_sync();
       }
-      if (more_q) q_there();
       if (pc.n_pieces > 1) {
         // the last block at the unit joins its pieces, in the blocks' order
         __threadfence();
@@ -644,7 +684,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!meet()) break;
         if (sh.last) {
           const int blocks = pc.c1 - pc.c0 + 1;
-          auto has = [&](int b) { return pc.mask[b >> 5] >> (b & 31) & 1; };
+          auto has = [&](int b) { return sh.mask[k & 1][b >> 5] >> (b & 31) & 1; };
           auto row_at = [&](int b) { return static_cast<int64_t>(b ? 2 * (pc.c0 + b) : pc.slot0) * (2 * kTile); };
           if (static_cast<int>(threadIdx.x) < n_rows) {  // a row's maximum and sum
             const int q = threadIdx.x;
@@ -673,16 +713,20 @@ __global__ void __launch_bounds__(kThreads, 1)
             float4 acc[kAt];
 #pragma unroll
             for (int e = 0; e < kAt; ++e) acc[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
             for (int b = 0; b < blocks; ++b) {
-              if (!has(b)) continue;
               float4 v[kAt];
               float f[kAt];
 #pragma unroll
               for (int e = 0; e < kAt; ++e) {
-                const int x = min(x0 + 256 * e, n_rows * (D / 4) - 1);
-                const int64_t at = row_at(b) + x / (D / 4);
-                v[e] = __ldcg(reinterpret_cast<const float4*>(A.part_o + at * D + x % (D / 4) * 4));
-                f[e] = __ldcg(&A.part_ml[at]).x;
+                v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+                f[e] = -INFINITY;
+                if (has(b)) {
+                  const int x = min(x0 + 256 * e, n_rows * (D / 4) - 1);
+                  const int64_t at = row_at(b) + x / (D / 4);
+                  v[e] = __ldcg(reinterpret_cast<const float4*>(A.part_o + at * D + x % (D / 4) * 4));
+                  f[e] = __ldcg(&A.part_ml[at]).x;
+                }
               }
 #pragma unroll
               for (int e = 0; e < kAt; ++e) {
@@ -980,52 +1024,58 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
     } else if (i == 2) {
       // ---------------------------------------------------------- what comes next
-      int64_t total = 0;
-      for (int s = lane; s < C.n_seq; s += 32) total += C.H * unit_cost(seq_span(C, A, s), A).head;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      int64_t total = group_sum;
+      if (C.n_seq > 32) {
+        total = 0;
+        for (int g = 0; g < C.n_seq; g += 32) {
+          load_group(g);
+          total += __shfl_sync(0xffffffffu, group_sum, 31);
+        }
+        load_group(0);
+      } else {
+        total = __shfl_sync(0xffffffffu, group_sum, 31);
+      }
       // shares of four steps at least
-      const int64_t n_cta = max(min(static_cast<int64_t>(gridDim.x), total / (4 * kTile * A.G)), static_cast<int64_t>(1));
-      const int64_t cta = blockIdx.x;
-      auto begin = [&](int64_t c) { return c * total / n_cta; };
+      const int n_cta = static_cast<int>(
+          max(min(static_cast<int64_t>(gridDim.x), quotient(total, 4 * kTile * A.G)), static_cast<int64_t>(1)));
+      const int cta = blockIdx.x;
+      // block c's share begins at c quotients and min(c, remainder)
+      const int64_t each = quotient(total, n_cta), extra = total - each * n_cta;
+      auto begin = [&](int c) { return c * each + min(static_cast<int64_t>(c), extra); };
+      auto block_of = [&](int64_t y) {
+        const bool early = y < extra * (each + 1);
+        return static_cast<int>(early ? 0 : extra) +
+               static_cast<int>(quotient(early ? y : y - extra * (each + 1), early ? each + 1 : each));
+      };
       int64_t x = cta < n_cta ? begin(cta) : total;
       const int64_t x0 = x, x1 = cta < n_cta ? begin(cta + 1) : total;
       int k = 0;
-      int64_t base = 0;  // cost before sequence group `group`
-      int group = 0;
+      int64_t base = 0;  // cost before the group of sequences
       while (ok) {
-        Piece pc;
-        pc.valid = 0;
-        while (x < x1) {
+        if (k > 1 && !wait(sh.piece_empty[k & 1], ((k >> 1) + 1) & 1)) break;
+        Piece& pc = sh.piece[k & 1];
+        bool found = false;
+        int64_t w0 = 0, w = 1, w1 = 0;
+        int steps = 1, slot = 0;
+        while (x < x1 && !found) {
           // the sequence of cost x
-          int64_t before = 0;
-          int seq = 0;
-          for (;; group += 32) {
-            const int s = group + lane;
-            const int64_t mine = s < C.n_seq ? C.H * unit_cost(seq_span(C, A, s), A).head : 0;
-            int64_t sum = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-              const int64_t v = __shfl_up_sync(0xffffffffu, sum, o);
-              if (lane >= o) sum += v;
-            }
-            const unsigned past = __ballot_sync(0xffffffffu, base + sum > x);
-            if (past || group + 32 >= C.n_seq) {
-              const int l = past ? __ffs(past) - 1 : 31;
-              seq = group + l;
-              before = base + __shfl_sync(0xffffffffu, sum - mine, l);
-              break;
-            }
-            base += __shfl_sync(0xffffffffu, sum, 31);
+          unsigned past;
+          while (!(past = __ballot_sync(0xffffffffu, base + group_sum > x)) && group + 32 < C.n_seq) {
+            base += __shfl_sync(0xffffffffu, group_sum, 31);
+            load_group(group + 32);
           }
-          if (seq >= C.n_seq) {
+          if (!past) {
             x = x1;
             break;
           }
-          const SeqSpan span = seq_span(C, A, seq);
+          const int sl = __ffs(past) - 1, seq = group + sl;
+          const int64_t before = base + __shfl_sync(0xffffffffu, group_sum - group_cost, sl);
+          const SeqSpan span = {__shfl_sync(0xffffffffu, group_span.first, sl), __shfl_sync(0xffffffffu, group_span.n, sl),
+                                __shfl_sync(0xffffffffu, group_span.kv, sl)};
+          // the unit of cost x
           const UnitCost u = unit_cost(span, A);
           auto upto = [&](int64_t at) { return at * u.w0 + u.dw * (at * (at - 1) / 2); };
-          const int h = static_cast<int>((x - before) / u.head);
+          const int h = static_cast<int>(quotient(x - before, u.head));
           const int64_t in_head = x - before - h * u.head;
           int lo = 0, hi = u.tiles - 1;
           while (lo < hi) {
@@ -1035,54 +1085,56 @@ __global__ void __launch_bounds__(kThreads, 1)
             else
               hi = mid - 1;
           }
-          const int64_t w0 = before + h * u.head + upto(lo), w = u.w0 + u.dw * lo, w1 = w0 + w;
-          pc.seq = seq, pc.first = span.first, pc.n = span.n, pc.kv = span.kv;
-          pc.h = h;
-          pc.r0 = lo * 2 * kTile;
-          pc.n_rows = static_cast<int>(min(static_cast<int64_t>(2 * kTile), static_cast<int64_t>(span.n) * A.G - pc.r0));
-          pc.kv_end = seen(span, A.causal, (pc.r0 + pc.n_rows - 1) / A.G);
-          const int all = (pc.kv_end + kTile - 1) / kTile, steps = max(all, 1);
+          w0 = before + h * u.head + upto(lo), w = u.w0 + u.dw * lo, w1 = w0 + w;
+          const int r0 = lo * 2 * kTile;
+          const int n_rows =
+              static_cast<int>(min(static_cast<int64_t>(2 * kTile), static_cast<int64_t>(span.n) * A.G - r0));
+          const int kv_end = seen(span, A.causal, (r0 + n_rows - 1) / A.G);
+          const int all = (kv_end + kTile - 1) / kTile;
+          steps = max(all, 1);
           const int p0 = cut(x, w0, w, steps), p1 = cut(min(x1, w1), w0, w, steps);
-          if (p0 < p1) {
-            pc.valid = 1;
-            pc.t0 = p0;
-            const int t1 = min(p1, all);
-            pc.dual = pc.n_rows <= kTile;
-            const int n = max(t1 - p0, 0);
-            if (pc.dual) {
-              pc.nt[0] = (n + 1) / 2;
-              pc.nt[1] = n / 2;
-              pc.n_ops = n;
-            } else {
-              const int end0 = (seen(span, A.causal, (pc.r0 + kTile - 1) / A.G) + kTile - 1) / kTile;
-              pc.nt[0] = max(min(end0, t1) - p0, 0);
-              pc.nt[1] = n;
-              pc.n_ops = n;
-            }
-            pc.c0 = static_cast<int>(((w0 + 1) * n_cta - 1) / total);
-            pc.c1 = static_cast<int>((w1 * n_cta - 1) / total);
-            pc.slot0 = 2 * pc.c0 + (begin(pc.c0) == w0 ? 0 : 1);
-            pc.slot = static_cast<int>(2 * cta) + (x == x0 ? 0 : 1);
-            pc.n_pieces = 0;
-#pragma unroll
-            for (int b = 0; b < kMaxBlocks; b += 32) {
-              const int64_t c = pc.c0 + b + lane;
-              const bool has = c <= pc.c1 && cut(max(begin(c), w0), w0, w, steps) < cut(min(begin(c + 1), w1), w0, w, steps);
-              pc.mask[b / 32] = __ballot_sync(0xffffffffu, has);
-              pc.n_pieces += __popc(pc.mask[b / 32]);
-            }
-          }
+          slot = 2 * cta + (x == x0 ? 0 : 1);
           x = w1;
-          if (pc.valid) break;
+          if (p0 >= p1) continue;
+          found = true;
+          const int n = max(min(p1, all) - p0, 0);
+          const bool dual = n_rows <= kTile;
+          if (lane == 0) {
+            pc.valid = 1;
+            pc.seq = seq, pc.first = span.first, pc.n = span.n, pc.kv = span.kv;
+            pc.h = h, pc.r0 = r0, pc.n_rows = n_rows;
+            pc.t0 = p0, pc.n_ops = n, pc.kv_end = kv_end, pc.dual = dual;
+            const int end0 = (seen(span, A.causal, (r0 + kTile - 1) / A.G) + kTile - 1) / kTile;
+            pc.nt[0] = dual ? (n + 1) / 2 : max(min(end0 - p0, n), 0);
+            pc.nt[1] = dual ? n / 2 : n;
+          }
         }
-        if (k > 1 && !wait(sh.piece_empty[k & 1], ((k >> 1) + 1) & 1)) break;
+        if (lane == 0 && !found) pc.valid = 0;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_addr(&sh.piece_full[k & 1]));
+        if (!found) break;
+        // Who else is at the unit: read after the next piece has been announced.
+        const int c0 = w0 >= x0 ? cta : block_of(w0), c1 = w1 <= x1 ? cta : block_of(w1 - 1);
+        int pieces = 1;
+        if (c0 != c1) {
+          pieces = 0;
+#pragma unroll 1
+          for (int c = c0; c <= c1; c += 32) {
+            const int64_t from = max(begin(c + lane), w0), to = min(begin(c + lane + 1), w1);
+            const unsigned has =
+                __ballot_sync(0xffffffffu, c + lane <= c1 && cut(from, w0, w, steps) < cut(to, w0, w, steps));
+            if (lane == 0) sh.mask[k & 1][(c - c0) / 32] = has;
+            pieces += __popc(has);
+          }
+        }
         if (lane == 0) {
-          sh.piece[k & 1] = pc;
-          mbar_arrive(smem_addr(&sh.piece_full[k & 1]));
+          pc.n_pieces = pieces;
+          pc.c0 = c0, pc.c1 = c1;
+          pc.slot0 = 2 * c0 + (begin(c0) == w0 ? 0 : 1);
+          pc.slot = slot;
         }
         __syncwarp();
         ++k;
-        if (!pc.valid) break;
       }
     }
   }
@@ -1143,8 +1195,9 @@ hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int box, cudaStr
   constexpr int kBytes = Smem<SRC, D>::kRest + static_cast<int>(sizeof(Shared<Smem<SRC, D>::kStages>));
   HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes),
               "hf_attend: shared memory size");
-  kern<<<std::min(device_sm_count(), kMaxBlocks), kThreads, kBytes, stream>>>(maps[0], maps[1], c, a, box);
-  HF_CUDA_TRY(cudaGetLastError(), "hf_attend: launch");
+  HF_CUDA_TRY(launch_dependent(kern, dim3(std::min(device_sm_count(), kMaxBlocks)), dim3(kThreads), kBytes, stream,
+                               maps[0], maps[1], c, a, box),
+              "hf_attend: launch");
   return HF_OK;
 }
 

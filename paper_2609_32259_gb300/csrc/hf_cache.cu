@@ -213,6 +213,8 @@ template <typename T, int KIND, int D>
 __global__ void __launch_bounds__(32 * kWarps) append_kernel(const CacheArgs C, const AppendArgs A) {
   using L = Lanes<D>;
   constexpr int NC = L::kChunks;
+  depend_wait();
+  depend_launch();
   const int lane = threadIdx.x & 31;
   const int tok = blockIdx.x * kWarps + (threadIdx.x >> 5);
   if (tok >= A.t.n_tok) return;
@@ -312,6 +314,8 @@ template <typename T, int KIND, int D>
 __global__ void __launch_bounds__(32 * kWarps) read_kernel(const CacheArgs C, const ReadArgs A) {
   using L = Lanes<D>;
   constexpr int NC = L::kChunks;
+  depend_wait();
+  depend_launch();
   const int lane = threadIdx.x & 31;
   const int tok = blockIdx.x * kWarps + (threadIdx.x >> 5);
   if (tok >= A.t.n_tok) return;
@@ -371,6 +375,8 @@ struct InvFreq {
 };
 
 __global__ void rope_table_kernel(const InvFreq inv, int half, int pos0, int64_t n, float2* out) {
+  depend_wait();
+  depend_launch();
   const int64_t i = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x;
   if (i >= n) return;
   float s, c;
@@ -390,14 +396,16 @@ dim3 token_grid(int n_tok, int heads) {
 
 template <typename T, int KIND, int D>
 hf_status launch_append(const CacheArgs& c, const AppendArgs& a, cudaStream_t stream) {
-  append_kernel<T, KIND, D><<<token_grid<D>(a.t.n_tok, 2 * c.H + a.H_q), 32 * kWarps, 0, stream>>>(c, a);
-  HF_CUDA_TRY(cudaGetLastError(), "hf_cache_append: launch");
+  HF_CUDA_TRY(launch_dependent(append_kernel<T, KIND, D>, token_grid<D>(a.t.n_tok, 2 * c.H + a.H_q), dim3(32 * kWarps),
+                               0, stream, c, a),
+              "hf_cache_append: launch");
   return HF_OK;
 }
 template <typename T, int KIND, int D>
 hf_status launch_read(const CacheArgs& c, const ReadArgs& a, cudaStream_t stream) {
-  read_kernel<T, KIND, D><<<token_grid<D>(a.t.n_tok, 2 * c.H), 32 * kWarps, 0, stream>>>(c, a);
-  HF_CUDA_TRY(cudaGetLastError(), "hf_cache_read: launch");
+  HF_CUDA_TRY(launch_dependent(read_kernel<T, KIND, D>, token_grid<D>(a.t.n_tok, 2 * c.H), dim3(32 * kWarps), 0, stream,
+                               c, a),
+              "hf_cache_read: launch");
   return HF_OK;
 }
 
@@ -455,9 +463,10 @@ extern "C" hf_status hf_rope_table(int32_t D, double theta, const float* h_inv_f
   }
   if (n_pos == 0) return HF_OK;
   const int64_t n = static_cast<int64_t>(n_pos) * (D / 2);
-  rope_table_kernel<<<static_cast<unsigned>((n + 255) / 256), 256, 0, reinterpret_cast<cudaStream_t>(stream_)>>>(
-      inv, D / 2, pos0, n, reinterpret_cast<float2*>(d_table));
-  HF_CUDA_TRY(cudaGetLastError(), "hf_rope_table: launch");
+  HF_CUDA_TRY(launch_dependent(rope_table_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0,
+                               reinterpret_cast<cudaStream_t>(stream_), inv, D / 2, pos0, n,
+                               reinterpret_cast<float2*>(d_table)),
+              "hf_rope_table: launch");
   return HF_OK;
 }
 
