@@ -87,6 +87,36 @@ __device__ __forceinline__ TilePlace find_tile(const CacheArgs& C, const AttendA
   return {C.n_seq, 0, 0};
 }
 
+// floor(x / d), x >= 0, d > 0: fp32 quotients, put right (a 64-bit division is
+// some hundred instructions).
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t d) {
+  int64_t q = 0, r = x;
+  const float inv = 1.f / static_cast<float>(d);
+  while (r < 0 || r >= d) {
+    const int64_t step = static_cast<int64_t>(static_cast<float>(r) * inv);
+    q += step != 0 ? step : r < 0 ? -1 : 1;
+    r = x - q * d;
+  }
+  return q;
+}
+
+// `total` shared out over `n` blocks: block c's share begins at c quotients and
+// min(c, remainder).
+struct Shares {
+  int64_t each, extra;
+  __device__ __forceinline__ Shares(int64_t total, int64_t n) {
+    each = quotient(total, n);
+    extra = total - each * n;
+  }
+  __device__ __forceinline__ int64_t begin(int64_t c) const { return c * each + min(c, extra); }
+  // The block whose share holds y (each > 0).
+  __device__ __forceinline__ int block_of(int64_t y) const {
+    const bool early = y < extra * (each + 1);
+    return static_cast<int>(early ? 0 : extra) +
+           static_cast<int>(quotient(early ? y : y - extra * (each + 1), early ? each + 1 : each));
+  }
+};
+
 // Tiles of `rows` flattened rows at most, over all sequences.
 inline int64_t most_tiles(int64_t n_tok, int G, int n_seq, int rows) {
   return n_tok * G / rows + (n_seq < n_tok ? n_seq : n_tok);

@@ -21,8 +21,8 @@
 // 4-bit rows stay codes: the nibbles c of a word are masked in place and are, as
 // bf16 numbers, c 2^-133 and 16 c 2^-133 (subnormal, exact), one or two
 // operations for two codes.  Queries are scaled by 2^64 (and 2^60), and group
-// scales apply to the 32-channel partial scores in fp32; for the values they go
-// into P (one rounding, the one that P takes anyway).  The offset of 8 is the
+// scales apply to the 32-channel partial scores in fp32; for the values they and
+// 2^64 go into P (one rounding, the one that P takes anyway).  The offset of 8 is the
 // score accumulator's start, -8 sum(q), and a further product with a constant
 // row for the values.
 #include <algorithm>
@@ -67,6 +67,14 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma16816_from(float (&d)[4], float c0, float c1, uint32_t a0, uint32_t a1, uint32_t a2,
+                                              uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%10, %11, %10, %11};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+}
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -99,7 +107,7 @@ struct Ring {
   static constexpr int kKs = 2 * kKeys * kRow;
   static constexpr int kVs = kKs + kKeys * kScale;
   static constexpr int kStage = kVs + kKeys * kScale;
-  static constexpr int kStages = kQ4 ? 4 : 3;            // D 128: 18 and 24 KB a warp
+  static constexpr int kStages = 3;                      // D 128: 14 and 24 KB a warp
   static constexpr int kWarpBytes = kStages * kStage;
   static constexpr int kStep = kKeys * kWarps;           // keys of a block's step
 };
@@ -120,9 +128,16 @@ __device__ __forceinline__ int chunk_at(int key, int c) {
 // t + 4, so that the four lanes t read neighbouring rows of values.
 __device__ __forceinline__ int kappa(int r) { return (r & 8) + ((r & 7) >> 1) + 4 * (r & 1); }
 
-// Blocks on an SM: what the registers allow; rings of 72 and 96 KB a block.
+// Blocks on an SM: what the registers and the rings (55 and 96 KB) allow.
 template <int KIND, int NT>
 constexpr int kBlocks = KIND == HF_CACHE_Q4 && NT == 1 ? 3 : 2;
+
+// Shared memory: the rings, and once they are empty the maxima and sums of a
+// unit's pieces, at most one a block.
+constexpr int kMaxSms = 160;
+template <int KIND, int D, int NT>
+constexpr int kRingBytes = std::max(kWarps * Ring<KIND, D>::kWarpBytes,
+                                    (2 * kMaxSms * kBlocks<KIND, NT> + 1) * 8 * NT * static_cast<int>(sizeof(float)));
 
 template <int KIND, int D, int NT>
 __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
@@ -131,11 +146,12 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
   constexpr bool kQ4 = R::kQ4;
   constexpr int KB = R::kKeys, S = R::kStages;
   constexpr int RB = 8 * NT;      // query rows of a unit
+  constexpr float kShift = kQ4 ? 64.f : 0.f;  // log2 of the factor in P (and in l)
   constexpr int NG = D / 32;
   constexpr int kOut = D + 4;     // pitch of a query's outputs in shared memory
   static_assert(RB * kOut * 4 <= R::kWarpBytes, "a warp's outputs fit its ring");
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int64_t s_pre[kMaxReq + 1];
+  int64_t* s_pre = reinterpret_cast<int64_t*>(smem + kRingBytes<KIND, D, NT>);  // n_seq + 1
   __shared__ int64_t s_warp[kWarps];
   __shared__ float s_m[kWarps][RB], s_l[kWarps][RB];
   __shared__ int s_last;
@@ -147,17 +163,28 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
   depend_wait();
   depend_launch();
   // Steps of the sequences before each one.
-  {
+  auto steps_of = [&](int i) {
+    if (i >= C.n_seq) return static_cast<int64_t>(0);
+    const SeqSpan sp = seq_span(C, A, i);
+    const int64_t chunks = (static_cast<int64_t>(sp.n) * A.G + RB - 1) / RB;
+    return chunks * C.H * max((sp.kv + R::kStep - 1) / R::kStep, 1);
+  };
+  if (C.n_seq <= 32) {  // every warp for itself: the same values
+    int64_t n = steps_of(lane);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, n, o);
+      if (lane >= o) n += v;
+    }
+    if (lane == 0) s_pre[0] = 0;
+    if (lane < C.n_seq) s_pre[lane + 1] = n;
+    __syncwarp();
+  } else {
     int64_t carry = 0;
     if (threadIdx.x == 0) s_pre[0] = 0;
     for (int base = 0; base < C.n_seq; base += kThreads) {
       const int i = base + threadIdx.x;
-      int64_t n = 0;
-      if (i < C.n_seq) {
-        const SeqSpan sp = seq_span(C, A, i);
-        const int64_t chunks = (static_cast<int64_t>(sp.n) * A.G + RB - 1) / RB;
-        n = chunks * C.H * max((sp.kv + R::kStep - 1) / R::kStep, 1);
-      }
+      int64_t n = steps_of(i);
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int64_t v = __shfl_up_sync(0xffffffffu, n, o);
@@ -175,11 +202,12 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
     }
   }
   const int64_t total = s_pre[C.n_seq];
-  const int64_t n_cta = min(static_cast<int64_t>(gridDim.x), total);
+  const int64_t n_cta = max(min(static_cast<int64_t>(gridDim.x), total), static_cast<int64_t>(1));
   const int64_t cta = blockIdx.x;
-  if (cta >= n_cta) return;
-  int64_t x = cta * total / n_cta;
-  const int64_t share0 = x, share1 = (cta + 1) * total / n_cta;
+  if (cta >= n_cta || total == 0) return;
+  const Shares shares(total, n_cta);
+  int64_t x = shares.begin(cta);
+  const int64_t share0 = x, share1 = shares.begin(cta + 1);
 
   while (x < share1) {
     // ---- the unit of step x, and this block's piece [p0, p1) of its steps
@@ -192,13 +220,51 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
     const SeqSpan span = seq_span(C, A, seq);
     const int chunks = static_cast<int>((static_cast<int64_t>(span.n) * A.G + RB - 1) / RB);
     const int steps = max((span.kv + R::kStep - 1) / R::kStep, 1);
-    const int64_t unit = (x - s_pre[seq]) / steps;
-    const int64_t u0 = s_pre[seq] + unit * steps, u1 = u0 + steps;
-    const int h = static_cast<int>(unit / chunks), r0 = static_cast<int>(unit % chunks) * RB;
+    const int unit = static_cast<int>(quotient(x - s_pre[seq], steps));
+    const int64_t u0 = s_pre[seq] + static_cast<int64_t>(unit) * steps, u1 = u0 + steps;
+    const int h = unit / chunks, r0 = (unit - h * chunks) * RB;
     const int p0 = static_cast<int>(x - u0), p1 = static_cast<int>(min(share1, u1) - u0);
     const int n_rows = static_cast<int>(min(static_cast<int64_t>(RB), static_cast<int64_t>(span.n) * A.G - r0));
     const int kv_end = seen(span, A.causal, (r0 + n_rows - 1) / A.G);
 
+    // ---- the warp's ring
+    const char* kb = C.k + (kQ4 ? static_cast<int64_t>(h) * C.rows * (D / 2) : h * C.head_stride * 2);
+    const char* vb = C.v + (kQ4 ? static_cast<int64_t>(h) * C.rows * (D / 2) : h * C.head_stride * 2);
+    const int64_t row_bytes = kQ4 ? D / 2 : C.row_stride * 2;
+    const char* ksb = C.ks + static_cast<int64_t>(h) * C.rows * (D / 16);
+    const char* vsb = C.vs + static_cast<int64_t>(h) * C.rows * (D / 16);
+    auto row_of = [&](int step) -> int {  // of key `lane` of this warp's step
+      const int key = step * R::kStep + warp * KB + lane;
+      return step < p1 && lane < KB && key < kv_end ? cache_row(C, seq, key) : -1;
+    };
+    auto issue = [&](int step, int stage, int row) {
+      if (step < p1) {
+        const uint32_t dst = ring_a + stage * R::kStage;
+        constexpr int kChunks = R::kRow / 16;
+#pragma unroll
+        for (int i = 0; i < KB * kChunks / 32; ++i) {
+          const int idx = i * 32 + lane, key = idx / kChunks, c = idx % kChunks;
+          const int r = __shfl_sync(0xffffffffu, row, key);
+          const int64_t at = max(r, 0) * row_bytes + c * 16;
+          const uint32_t d = dst + chunk_at<KIND, D>(key, c);
+          cp_async_16_or_zero(d, kb + at, r >= 0);
+          cp_async_16_or_zero(d + R::kV, vb + at, r >= 0);
+        }
+        if constexpr (kQ4) {
+          const int64_t at = static_cast<int64_t>(max(row, 0)) * R::kScale;
+          cp_async_small<R::kScale>(dst + R::kKs + lane * R::kScale, ksb + at, row >= 0);
+          cp_async_small<R::kScale>(dst + R::kVs + lane * R::kScale, vsb + at, row >= 0);
+        }
+      }
+      cp_async_commit();
+    };
+
+    int rows[S];  // looked up side by side
+#pragma unroll
+    for (int i = 0; i < S; ++i) rows[i] = row_of(p0 + i);
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) issue(p0 + i, i, rows[i]);
+    int row = rows[S - 1];
     // ---- queries
     uint32_t qf[NT][D / 16][2];
     float q_off[kQ4 ? NT : 1][kQ4 ? NG : 1][2];
@@ -250,41 +316,13 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
       }
     }
     const float scale = kQ4 ? A.scale_log2 * 590295810358705651712.f : A.scale_log2;  // 2^69
-
-    // ---- the warp's ring
-    const char* kb = C.k + (kQ4 ? static_cast<int64_t>(h) * C.rows * (D / 2) : h * C.head_stride * 2);
-    const char* vb = C.v + (kQ4 ? static_cast<int64_t>(h) * C.rows * (D / 2) : h * C.head_stride * 2);
-    const int64_t row_bytes = kQ4 ? D / 2 : C.row_stride * 2;
-    const char* ksb = C.ks + static_cast<int64_t>(h) * C.rows * (D / 16);
-    const char* vsb = C.vs + static_cast<int64_t>(h) * C.rows * (D / 16);
-    auto row_of = [&](int step) -> int {  // of key `lane` of this warp's step
-      const int key = step * R::kStep + warp * KB + lane;
-      return step < p1 && lane < KB && key < kv_end ? cache_row(C, seq, key) : -1;
-    };
-    auto issue = [&](int step, int stage, int row) {
-      if (step < p1) {
-        const uint32_t dst = ring_a + stage * R::kStage;
-        constexpr int kChunks = R::kRow / 16;
-#pragma unroll
-        for (int i = 0; i < KB * kChunks / 32; ++i) {
-          const int idx = i * 32 + lane, key = idx / kChunks, c = idx % kChunks;
-          const int r = __shfl_sync(0xffffffffu, row, key);
-          const int64_t at = max(r, 0) * row_bytes + c * 16;
-          const uint32_t d = dst + chunk_at<KIND, D>(key, c);
-          cp_async_16_or_zero(d, kb + at, r >= 0);
-          cp_async_16_or_zero(d + R::kV, vb + at, r >= 0);
-        }
-        if constexpr (kQ4) {
-          const int64_t at = static_cast<int64_t>(max(row, 0)) * R::kScale;
-          cp_async_small<R::kScale>(dst + R::kKs + lane * R::kScale, ksb + at, row >= 0);
-          cp_async_small<R::kScale>(dst + R::kVs + lane * R::kScale, vsb + at, row >= 0);
-        }
-      }
-      cp_async_commit();
-    };
+    const float inv_scale = 1.f / scale;
+    const int all_see = seen(span, A.causal, r0 / A.G);  // by the first row, so by all
 
     float o[NT][D / 16][4], o_off[kQ4 ? NT : 1][kQ4 ? NG : 1][4];
-    float m[NT][2], l[NT][2];
+    // m: the maximum, scaled; reach: the largest score that moves nothing; neg: what
+    // is added to a scaled score before the power
+    float m[NT][2], l[NT][2], reach[NT][2], neg[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -297,13 +335,11 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
 #pragma unroll
           for (int e = 0; e < 4; ++e) o_off[nt][i][e] = 0.f;
       }
-      m[nt][0] = m[nt][1] = -INFINITY;
+      m[nt][0] = m[nt][1] = reach[nt][0] = reach[nt][1] = -INFINITY;
+      neg[nt][0] = neg[nt][1] = 0.f;
       l[nt][0] = l[nt][1] = 0.f;
     }
 
-#pragma unroll
-    for (int i = 0; i < S - 1; ++i) issue(p0 + i, i, row_of(p0 + i));
-    int row = row_of(p0 + S - 1);
     int stage = 0, ahead = S - 1;
     for (int step = p0; step < p1; ++step) {
       cp_async_wait<S - 2>();
@@ -346,9 +382,9 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
             const float f0 = bf16_half(sc[0][gr / 2], gr & 1), f1 = bf16_half(sc[1][gr / 2], gr & 1);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              float c[4] = {q_off[nt][gr][0], q_off[nt][gr][1], q_off[nt][gr][0], q_off[nt][gr][1]};
-              mma16816(c, c8[0] & 0x000f000fu, c8[1] & 0x000f000fu, d8[0] & 0x000f000fu, d8[1] & 0x000f000fu,
-                       qf[nt][2 * gr][0], qf[nt][2 * gr][1]);
+              float c[4];
+              mma16816_from(c, q_off[nt][gr][0], q_off[nt][gr][1], c8[0] & 0x000f000fu, c8[1] & 0x000f000fu,
+                            d8[0] & 0x000f000fu, d8[1] & 0x000f000fu, qf[nt][2 * gr][0], qf[nt][2 * gr][1]);
               mma16816(c, c8[0] & 0x00f000f0u, c8[1] & 0x00f000f0u, d8[0] & 0x00f000f0u, d8[1] & 0x00f000f0u,
                        qf[nt][2 * gr + 1][0], qf[nt][2 * gr + 1][1]);
               s[nt][0] = fmaf(f0, c[0], s[nt][0]);
@@ -377,16 +413,20 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[nt][e] += s2[nt][e];
         }
-        // what is not seen, and the running maximum
+        // what is not seen, and the running maximum (of scores before scaling)
         const int ka = key0 + 16 * b + (kQ4 ? kappa(g) : g), kb8 = ka + 8;
         bool past = false;
+        if (key0 + 16 * b + 16 > all_see) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if ((e < 2 ? ka : kb8) >= lim[nt][e & 1]) s[nt][e] = -INFINITY;
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s[nt][e] = (e < 2 ? ka : kb8) < lim[nt][e & 1] ? s[nt][e] * scale : -INFINITY;
-            past |= s[nt][e] > m[nt][e & 1] + kStretch;
-          }
+          for (int e = 0; e < 2; ++e) past |= fmaxf(s[nt][e], s[nt][e + 2]) > reach[nt][e];
         if (__any_sync(0xffffffffu, past)) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
@@ -396,9 +436,11 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-              const float next = fmaxf(m[nt][e], top);
+              const float next = fmaxf(m[nt][e], top * scale);
               const float fix = next == -INFINITY ? 1.f : exp2_approx(m[nt][e] - next);
               m[nt][e] = next;
+              reach[nt][e] = next == -INFINITY ? next : (next + kStretch) * inv_scale;
+              neg[nt][e] = next == -INFINITY ? 0.f : kShift - next;
               l[nt][e] *= fix;
 #pragma unroll
               for (int i = 0; i < D / 16; ++i) {
@@ -418,8 +460,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float top = m[nt][e & 1];
-            s[nt][e] = exp2_approx(s[nt][e] - (top == -INFINITY ? 0.f : top));
+            s[nt][e] = exp2_approx(fmaf(s[nt][e], scale, neg[nt][e & 1]));
             l[nt][e & 1] += s[nt][e];
           }
         // outputs
@@ -433,8 +474,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
               lds_words<1>(st + R::kV + chunk_at<KIND, D>(16 * b + t + 4 * e, g >> 2) + 4 * (g & 3), w[e]);
 #pragma unroll
           for (int gr = 0; gr < NG; ++gr) {
-            const float b64 = 18446744073709551616.f;  // 2^64
-            const float f0 = bf16_half(vs[0][gr / 2], gr & 1) * b64, f1 = bf16_half(vs[1][gr / 2], gr & 1) * b64;
+            const float f0 = bf16_half(vs[0][gr / 2], gr & 1), f1 = bf16_half(vs[1][gr / 2], gr & 1);
             const uint32_t c8 = __byte_perm(w[0][gr / 2], w[1][gr / 2], gr & 1 ? 0x7632 : 0x5410);
             const uint32_t e8 = __byte_perm(w[2][gr / 2], w[3][gr / 2], gr & 1 ? 0x7632 : 0x5410);
             const uint32_t d8 = c8 >> 8, g8 = e8 >> 8;
@@ -483,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
         const int q = 8 * nt + 2 * t + e;
         if (g == 0) {
           s_m[warp][q] = m[nt][e];
-          s_l[warp][q] = sum;
+          s_l[warp][q] = sum * (kQ4 ? 5.421010862427522e-20f : 1.f);  // 2^-64
         }
         float* dst = so + q * kOut;
         if constexpr (kQ4) {
@@ -510,7 +550,8 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
     const bool whole = p0 == 0 && p1 == steps;
     // A unit's pieces lie in blocks c0 .. c1; a block's first piece is its slot 0,
     // another one that it shares its slot 1.
-    const int64_t c0 = ((u0 + 1) * n_cta - 1) / total, c1 = (u1 * n_cta - 1) / total;
+    const int c0 = whole || u0 >= share0 ? static_cast<int>(cta) : shares.block_of(u0);
+    const int c1 = whole || u1 <= share1 ? static_cast<int>(cta) : shares.block_of(u1 - 1);
     const int64_t slot = 2 * cta + (x == share0 ? 0 : 1);
     for (int i = threadIdx.x; i < n_rows * (D / 4); i += kThreads) {
       const int q = i / (D / 4), c = i % (D / 4) * 4;
@@ -547,44 +588,63 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
     }
     if (!whole) {
       // the last block at the unit joins its pieces, in the blocks' order
-      __threadfence();
       __syncthreads();
       if (threadIdx.x == 0) {
-        const int done = atomicAdd(A.zeroed + c0, 1);
-        s_last = done == static_cast<int>(c1 - c0);
-        if (s_last) A.zeroed[c0] = 0;
         __threadfence();
+        s_last = atomicAdd(A.zeroed + c0, 1) == c1 - c0;
+        if (s_last) {
+          A.zeroed[c0] = 0;
+          __threadfence();
+        }
       }
       __syncthreads();
       if (s_last) {
+        const int first = 2 * c0 + (shares.begin(c0) == u0 ? 0 : 1), pieces = c1 - c0 + 1;
+        auto row_at = [&](int b) { return static_cast<int64_t>(b == 0 ? first : 2 * (c0 + b)) * RB; };
+        // weights of the pieces' rows, where the rings were: [piece][row]
+        float* sw = reinterpret_cast<float*>(smem);
+        float* stat = reinterpret_cast<float*>(smem) + pieces * RB;  // sums of a row, log-sums
+        for (int i = threadIdx.x; i < pieces * RB; i += kThreads) {
+          const float2 ml = __ldcg(&A.part_ml[row_at(i / RB) + i % RB]);
+          sw[i] = ml.x;
+          sw[i + pieces * RB + RB] = ml.y;
+        }
+        __syncthreads();
+        if (threadIdx.x < n_rows) {
+          float top = -INFINITY, sum = 0.f;
+          for (int b = 0; b < pieces; ++b) top = fmaxf(top, sw[b * RB + threadIdx.x]);
+          const float base = top == -INFINITY ? 0.f : top;
+          for (int b = 0; b < pieces; ++b) {
+            const float f = exp2_approx(sw[b * RB + threadIdx.x] - base);
+            sw[b * RB + threadIdx.x] = f;
+            sum = fmaf(sw[(b + pieces) * RB + RB + threadIdx.x], f, sum);
+          }
+          stat[threadIdx.x] = sum == 0.f ? 0.f : 1.f / sum;
+          if (A.lse) {
+            const int rr = r0 + threadIdx.x;
+            A.lse[(span.first + rr / A.G) * static_cast<int64_t>(A.H_q) + h * A.G + rr % A.G] =
+                (top + log2f(sum)) * 0.693147180559945309f;
+          }
+        }
+        __syncthreads();
         for (int i = threadIdx.x; i < n_rows * (D / 4); i += kThreads) {
           const int q = i / (D / 4), c = i % (D / 4) * 4;
-          const int64_t first = 2 * c0 + (c0 * total / n_cta == u0 ? 0 : 1);
-          float top = -INFINITY;
-          for (int64_t b = c0; b <= c1; ++b) top = fmaxf(top, __ldcg(&A.part_ml[(b == c0 ? first : 2 * b) * RB + q]).x);
-          const float base = top == -INFINITY ? 0.f : top;
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-          float sum = 0.f;
-#pragma unroll 4
-          for (int64_t b = c0; b <= c1; ++b) {
-            const int64_t at = (b == c0 ? first : 2 * b) * RB + q;
-            const float2 ml = __ldcg(&A.part_ml[at]);
-            const float f = exp2_approx(ml.x - base);
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(A.part_o + at * D + c));
-            sum = fmaf(ml.y, f, sum);
+#pragma unroll 8
+          for (int b = 0; b < pieces; ++b) {
+            const float f = sw[b * RB + q];
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(A.part_o + (row_at(b) + q) * D + c));
             acc.x = fmaf(v.x, f, acc.x);
             acc.y = fmaf(v.y, f, acc.y);
             acc.z = fmaf(v.z, f, acc.z);
             acc.w = fmaf(v.w, f, acc.w);
           }
           const int rr = r0 + q;
-          const int64_t tok = span.first + rr / A.G;
-          const int hq = h * A.G + rr % A.G;
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(A.out) + tok * A.o_row + hq * A.o_head + c;
+          const float inv = stat[q];
+          __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(A.out) +
+                               static_cast<int64_t>(span.first + rr / A.G) * A.o_row + (h * A.G + rr % A.G) * A.o_head + c;
           *reinterpret_cast<uint2*>(dst) =
               make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-          if (A.lse && c == 0) A.lse[tok * A.H_q + hq] = (top + log2f(sum)) * 0.693147180559945309f;
         }
       }
     }
@@ -596,10 +656,10 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
 template <int KIND, int D, int NT>
 hf_status launch_rows(const CacheArgs& c, const AttendArgs& a, cudaStream_t stream) {
   auto kern = attend_rows_kernel<KIND, D, NT>;
-  constexpr int smem = Ring<KIND, D>::kWarpBytes * kWarps;
+  const int smem = kRingBytes<KIND, D, NT> + 8 * (c.n_seq + 1);
   HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem),
               "hf_attend: shared memory size");
-  HF_CUDA_TRY(launch_dependent(kern, dim3(device_sm_count() * kBlocks<KIND, NT>), dim3(kThreads), smem, stream, c, a),
+  HF_CUDA_TRY(launch_dependent(kern, dim3(std::min(device_sm_count(), kMaxSms) * kBlocks<KIND, NT>), dim3(kThreads), smem, stream, c, a),
               "hf_attend: launch");
   return HF_OK;
 }

@@ -313,19 +313,6 @@ __device__ __forceinline__ int cut(int64_t x, int64_t w0, int64_t w, int n) {
   const int p = static_cast<int>(static_cast<float>(x - w0) / static_cast<float>(w) * n);
   return p < 2 ? 0 : p > n - 2 ? n : p;
 }
-// floor(x / d), x >= 0, d > 0: fp32 quotients, put right (a 64-bit division is
-// some hundred instructions).
-__device__ __forceinline__ int64_t quotient(int64_t x, int64_t d) {
-  int64_t q = 0, r = x;
-  const float inv = 1.f / static_cast<float>(d);
-  while (r < 0 || r >= d) {
-    const int64_t step = static_cast<int64_t>(static_cast<float>(r) * inv);
-    q += step != 0 ? step : r < 0 ? -1 : 1;
-    r = x - q * d;
-  }
-  return q;
-}
-
 template <int SRC, int D>
 struct Smem {
   static constexpr int kPart = kTile * 128;           // 128 rows of 64 channels
@@ -674,12 +661,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (pc.n_pieces > 1) {
         // the last block at the unit joins its pieces, in the blocks' order
-        __threadfence();
         if (!meet()) break;
         if (threadIdx.x == 0) {
-          sh.last = atomicAdd(A.zeroed + pc.c0, 1) == pc.n_pieces - 1;
-          if (sh.last) A.zeroed[pc.c0] = 0;
           __threadfence();
+          sh.last = atomicAdd(A.zeroed + pc.c0, 1) == pc.n_pieces - 1;
+          if (sh.last) {
+            A.zeroed[pc.c0] = 0;
+            __threadfence();
+          }
         }
         if (!meet()) break;
         if (sh.last) {
@@ -1039,14 +1028,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int n_cta = static_cast<int>(
           max(min(static_cast<int64_t>(gridDim.x), quotient(total, 4 * kTile * A.G)), static_cast<int64_t>(1)));
       const int cta = blockIdx.x;
-      // block c's share begins at c quotients and min(c, remainder)
-      const int64_t each = quotient(total, n_cta), extra = total - each * n_cta;
-      auto begin = [&](int c) { return c * each + min(static_cast<int64_t>(c), extra); };
-      auto block_of = [&](int64_t y) {
-        const bool early = y < extra * (each + 1);
-        return static_cast<int>(early ? 0 : extra) +
-               static_cast<int>(quotient(early ? y : y - extra * (each + 1), early ? each + 1 : each));
-      };
+      const Shares shares(total, n_cta);
+      auto begin = [&](int c) { return shares.begin(c); };
       int64_t x = cta < n_cta ? begin(cta) : total;
       const int64_t x0 = x, x1 = cta < n_cta ? begin(cta + 1) : total;
       int k = 0;
@@ -1114,7 +1097,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) mbar_arrive(smem_addr(&sh.piece_full[k & 1]));
         if (!found) break;
         // Who else is at the unit: read after the next piece has been announced.
-        const int c0 = w0 >= x0 ? cta : block_of(w0), c1 = w1 <= x1 ? cta : block_of(w1 - 1);
+        const int c0 = w0 >= x0 ? cta : shares.block_of(w0), c1 = w1 <= x1 ? cta : shares.block_of(w1 - 1);
         int pieces = 1;
         if (c0 != c1) {
           pieces = 0;
