@@ -407,13 +407,15 @@ def rope_table(D: int, table, theta: float = 0.0, inv_freq=None, pos0: int = 0,
 
 
 def cache_append(cache: CacheDesc, desc: AppendDesc, stream=None) -> None:
-    _check(lib().hf_cache_append(ctypes.byref(cache), ctypes.byref(desc), _stream(stream)),
-           "hf_cache_append")
+    st = lib().hf_cache_append(ctypes.byref(cache), ctypes.byref(desc), _stream(stream))
+    if st:
+        _check(st, "hf_cache_append")
 
 
 def cache_read(cache: CacheDesc, desc: ReadDesc, stream=None) -> None:
-    _check(lib().hf_cache_read(ctypes.byref(cache), ctypes.byref(desc), _stream(stream)),
-           "hf_cache_read")
+    st = lib().hf_cache_read(ctypes.byref(cache), ctypes.byref(desc), _stream(stream))
+    if st:
+        _check(st, "hf_cache_read")
 
 
 def attend_workspace_size(cache: CacheDesc) -> int:
@@ -428,8 +430,10 @@ def attend(cache: CacheDesc, desc: AttendDesc, workspace, workspace_bytes=None,
     """hf_attend; workspace_bytes None: the workspace tensor's bytes."""
     if workspace_bytes is None:
         workspace_bytes = int(workspace.numel() * workspace.element_size())
-    _check(lib().hf_attend(ctypes.byref(cache), ctypes.byref(desc), _dptr(workspace),
-                           workspace_bytes, _stream(stream)), "hf_attend")
+    st = lib().hf_attend(ctypes.byref(cache), ctypes.byref(desc), _dptr(workspace), workspace_bytes,
+                         _stream(stream))
+    if st:
+        _check(st, "hf_attend")
 
 
 def transfer_noalloc(desc: Desc, sender_kv, receiver_kv, stream=None) -> None:

@@ -173,25 +173,38 @@ def rope_table(n_pos: int, D: int, *, theta: float = 0.0, inv_freq=None, pos0: i
 
 
 def _stream_of(t: torch.Tensor, stream):
-    return torch.cuda.current_stream(t.device) if stream is None else stream
+    """The raw handle of `stream`, or of torch's current stream on t's device."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(t.device.index)
+    return stream
 
 
 def _rows(name, t, n, heads, D, dtype):
     """Row and head stride of a [n, heads, D] tensor whose channels are dense."""
-    if t.shape != (n, heads, D) or t.dtype != dtype or (D > 1 and n * heads > 0 and t.stride(2) != 1):
+    rows, hs, one = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if (t.dtype is not dtype or t.shape != (n, heads, D) or (one != 1 and n * heads > 0)
+            or (rows <= 0 and n > 1) or (hs <= 0 and heads > 1)):
         raise ValueError(f"{name} must be {dtype} [{n}, {heads}, {D}] with dense channels, got "
                          f"{t.dtype} {tuple(t.shape)} with strides {t.stride()}")
-    return t.stride(0), t.stride(1)
+    return rows, hs
 
 
 def _ints(name, t, n):
-    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous():
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor of {n} values")
     return t.data_ptr()
 
 
 _TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
 _NAMES = {v: k for k, v in _TORCH.items()}
+
+
+class _Codes(dict):
+    def __missing__(self, dtype):
+        raise ValueError(f"no cache takes {dtype}: bf16 or fp32")
+
+
+_CODES = _Codes({v: B.DTYPES[k] for k, v in _TORCH.items()})
 
 
 class KVCache:
@@ -207,16 +220,20 @@ class KVCache:
              (None: 0, one sequence)
     rows     rows to allocate when no buffers are given
 
+    workspace  of attend_workspace, shared with other caches whose attend calls
+             run in order with this one's (None: one of its own, made by the first
+             attend call, which waits for it)
+
     Calls run on `stream` (None: torch's current stream) and return at once;
-    status() waits and returns the HF_CHECK_* bits that they left.  The workspace
-    of attend is the cache's: its attend calls belong on one stream, or in order.
+    status() waits and returns the HF_CHECK_* bits that they left.  The attend
+    calls of one workspace belong on one stream, or in order.
     """
 
     def __init__(self, *, kind: str, H: int, D: int, n_seq: int, layers: int = 1,
                  kv: Optional[torch.Tensor] = None, codes: Optional[torch.Tensor] = None,
                  scales: Optional[torch.Tensor] = None, rows: Optional[int] = None,
                  block_table: Optional[torch.Tensor] = None, block_size: int = 0,
-                 row0: Optional[torch.Tensor] = None, device="cuda"):
+                 row0: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, device="cuda"):
         self.kind, self.H, self.D, self.n_seq = kind, int(H), int(D), int(n_seq)
         B.CACHE_KINDS[kind]
         if kind == "q4":
@@ -246,7 +263,7 @@ class KVCache:
         self.rows = int(rows)
         self.block_table, self.row0 = block_table, row0
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
-        self._workspace: Optional[torch.Tensor] = None
+        self._workspace = workspace
         max_blocks = 0
         if block_table is not None:
             max_blocks = block_table.shape[1]
@@ -269,7 +286,8 @@ class KVCache:
 
     @classmethod
     def of_tensors(cls, k: torch.Tensor, v: torch.Tensor, *, n_seq: int = 1,
-                   row0: Optional[torch.Tensor] = None) -> "KVCache":
+                   row0: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None) -> "KVCache":
         """One layer's keys and values [rows, H, D] where they are (slices of a
         larger tensor, with the same strides), for prompts that need no cache."""
         self = cls.__new__(cls)
@@ -281,7 +299,7 @@ class KVCache:
         self.kv, self.codes, self.scales, self.device = (k, v), None, None, k.device
         self.block_table, self.row0 = None, row0
         self._status = torch.zeros(1, dtype=torch.int32, device=k.device)
-        self._workspace = None
+        self._workspace = workspace
         if row0 is not None:
             _ints("row0", row0, n_seq)
         self._descs = [B.CacheDesc(kind=B.CACHE_KINDS[self.kind], H=H, D=D, n_seq=n_seq, rows=rows,
@@ -309,42 +327,47 @@ class KVCache:
         start[s] .. of the sequences; keys, and queries q [n_tok, H_q, D] into
         q_out, normed (k_norm, q_norm fp32 [D]) and rotated (rope, see
         rope_table) on the way."""
-        n, n_seq = k.shape[0], self.n_seq
-        dt = k.dtype
-        d = B.AppendDesc(dtype=B.DTYPES[_NAMES[dt]], n_tok=n, d_tok_ptr=_ints("tok_ptr", tok_ptr, n_seq + 1),
-                         d_start=_ints("start", start, n_seq), d_k=k.data_ptr(), d_v=v.data_ptr(), eps=eps)
-        d.k_row_stride, d.k_head_stride = _rows("k", k, n, self.H, self.D, dt)
-        d.v_row_stride, d.v_head_stride = _rows("v", v, n, self.H, self.D, dt)
+        n, n_seq, H, D, dt = k.shape[0], self.n_seq, self.H, self.D, k.dtype
+        k_row, k_head = _rows("k", k, n, H, D, dt)
+        v_row, v_head = _rows("v", v, n, H, D, dt)
+        H_q = d_q = d_q_out = q_row = q_head = 0
         if q is not None:
             if q_out is None:
                 raise ValueError("q needs q_out")
-            d.H_q = q.shape[1]
-            d.d_q, d.d_q_out = q.data_ptr(), q_out.data_ptr()
-            d.q_row_stride, d.q_head_stride = _rows("q", q, n, d.H_q, self.D, dt)
-            if _rows("q_out", q_out, n, d.H_q, self.D, dt) != (d.q_row_stride, d.q_head_stride):
+            H_q = q.shape[1]
+            q_row, q_head = _rows("q", q, n, H_q, D, dt)
+            if _rows("q_out", q_out, n, H_q, D, dt) != (q_row, q_head):
                 raise ValueError("q and q_out must have the same strides")
+            d_q, d_q_out = q.data_ptr(), q_out.data_ptr()
+        d_rope = rope_len = 0
         if rope is not None:
-            if rope.dtype != torch.float32 or rope.shape[1:] != (self.D // 2, 2) or not rope.is_contiguous():
+            rope_len = rope.shape[0]
+            if rope.dtype is not torch.float32 or rope.shape != (rope_len, D // 2, 2) or not rope.is_contiguous():
                 raise ValueError("rope must be a contiguous fp32 tensor [n_pos, D/2, 2]")
-            d.d_rope, d.rope_len = rope.data_ptr(), rope.shape[0]
-        if pos0 is not None:
-            d.d_pos0 = _ints("pos0", pos0, n_seq)
+            d_rope = rope.data_ptr()
         for name, w in (("k_norm", k_norm), ("q_norm", q_norm)):
-            if w is not None:
-                if w.dtype != torch.float32 or w.numel() != self.D or not w.is_contiguous():
-                    raise ValueError(f"{name} must be a contiguous fp32 tensor of {self.D} values")
-                setattr(d, "d_" + name, w.data_ptr())
-        B.cache_append(self._descs[layer], d, _stream_of(k, stream))
+            if w is not None and (w.dtype is not torch.float32 or w.numel() != D or not w.is_contiguous()):
+                raise ValueError(f"{name} must be a contiguous fp32 tensor of {D} values")
+        B.cache_append(
+            self._descs[layer],
+            B.AppendDesc(_CODES[dt], n, _ints("tok_ptr", tok_ptr, n_seq + 1), _ints("start", start, n_seq),
+                         k.data_ptr(), v.data_ptr(), k_row, k_head, v_row, v_head, H_q, d_q, d_q_out, q_row, q_head,
+                         d_rope, rope_len, None if pos0 is None else _ints("pos0", pos0, n_seq),
+                         None if k_norm is None else k_norm.data_ptr(),
+                         None if q_norm is None else q_norm.data_ptr(), eps),
+            _stream_of(k, stream))
 
     def read(self, layer: int, k, v, tok_ptr, start, *, stream=None) -> None:
         """hf_cache_read: rows start[s] .. of the sequences into packed k, v
         [n_tok, H, D]."""
-        n = k.shape[0]
-        d = B.ReadDesc(dtype=B.DTYPES[_NAMES[k.dtype]], n_tok=n, d_tok_ptr=_ints("tok_ptr", tok_ptr, self.n_seq + 1),
-                       d_start=_ints("start", start, self.n_seq), d_k=k.data_ptr(), d_v=v.data_ptr())
-        d.k_row_stride, d.k_head_stride = _rows("k", k, n, self.H, self.D, k.dtype)
-        d.v_row_stride, d.v_head_stride = _rows("v", v, n, self.H, self.D, k.dtype)
-        B.cache_read(self._descs[layer], d, _stream_of(k, stream))
+        n, dt = k.shape[0], k.dtype
+        k_row, k_head = _rows("k", k, n, self.H, self.D, dt)
+        v_row, v_head = _rows("v", v, n, self.H, self.D, dt)
+        B.cache_read(
+            self._descs[layer],
+            B.ReadDesc(_CODES[dt], n, _ints("tok_ptr", tok_ptr, self.n_seq + 1), _ints("start", start, self.n_seq),
+                       k.data_ptr(), v.data_ptr(), k_row, k_head, v_row, v_head),
+            _stream_of(k, stream))
 
     def attend(self, layer: int, q, out, q_ptr, kv_len, *, max_q_len: Optional[int] = None,
                max_kv_len: Optional[int] = None, causal: bool = True, scale: float = 0.0, lse=None,
@@ -353,22 +376,20 @@ class KVCache:
         s: q_ptr[s] .. q_ptr[s+1]) over the first kv_len[s] rows of their
         sequences; max_q_len and max_kv_len are upper bounds known on the host
         (None: what the packed tokens and the cache allow); lse fp32 [n_tok, H_q]."""
-        n, H_q = q.shape[0], q.shape[1]
-        d = B.AttendDesc(dtype=B.DTYPES[_NAMES[q.dtype]], H_q=H_q, n_tok=n,
-                         d_q_ptr=_ints("q_ptr", q_ptr, self.n_seq + 1),
-                         d_kv_len=_ints("kv_len", kv_len, self.n_seq),
-                         max_q_len=n if max_q_len is None else max_q_len,
-                         max_kv_len=self.rows if max_kv_len is None else max_kv_len,
-                         causal=int(bool(causal)), scale=scale, d_q=q.data_ptr(), d_out=out.data_ptr())
-        d.q_row_stride, d.q_head_stride = _rows("q", q, n, H_q, self.D, q.dtype)
-        d.out_row_stride, d.out_head_stride = _rows("out", out, n, H_q, self.D, q.dtype)
-        if lse is not None:
-            if lse.dtype != torch.float32 or lse.shape != (n, H_q) or not lse.is_contiguous():
-                raise ValueError("lse must be a contiguous fp32 tensor [n_tok, H_q]")
-            d.d_lse = lse.data_ptr()
+        n, H_q, D, dt = q.shape[0], q.shape[1], self.D, q.dtype
+        q_row, q_head = _rows("q", q, n, H_q, D, dt)
+        o_row, o_head = _rows("out", out, n, H_q, D, dt)
+        if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (n, H_q) or not lse.is_contiguous()):
+            raise ValueError("lse must be a contiguous fp32 tensor [n_tok, H_q]")
         if self._workspace is None:
             self._workspace = attend_workspace(self._descs[0], self.device)
-        B.attend(self._descs[layer], d, self._workspace, None, _stream_of(q, stream))
+        B.attend(
+            self._descs[layer],
+            B.AttendDesc(_CODES[dt], H_q, n, _ints("q_ptr", q_ptr, self.n_seq + 1), _ints("kv_len", kv_len, self.n_seq),
+                         n if max_q_len is None else max_q_len, self.rows if max_kv_len is None else max_kv_len,
+                         1 if causal else 0, scale, q.data_ptr(), out.data_ptr(), q_row, q_head, o_row, o_head,
+                         None if lse is None else lse.data_ptr()),
+            self._workspace.data_ptr(), self._workspace.numel(), _stream_of(q, stream))
 
     def status(self) -> int:
         """HF_CHECK_* bits of the calls so far (waits for the device)."""
@@ -376,9 +397,12 @@ class KVCache:
 
 
 def attend_workspace(desc: B.CacheDesc, device="cuda") -> torch.Tensor:
-    """A workspace for hf_attend (its counters zeroed)."""
+    """A workspace for hf_attend, its counters zeroed (and that waited for, so that
+    any stream may use it)."""
     ws = torch.empty(B.attend_workspace_size(desc), dtype=torch.uint8, device=device)
     ws[:B.ATTEND_ZEROED].zero_()
+    if not torch.cuda.is_current_stream_capturing():
+        torch.cuda.current_stream(ws.device).synchronize()
     return ws
 
 

@@ -129,6 +129,10 @@ def test_tensors_of_the_wrong_kind():
     with pytest.raises(ValueError):
         c.append(0, k, k.transpose(0, 1), i, i[:1])
     with pytest.raises(ValueError):
+        c.append(0, k[:, :1].expand(3, 2, 64), k, i, i[:1])  # one head's row for both
+    with pytest.raises(ValueError):
+        c.append(0, k.half(), k.half(), i, i[:1])
+    with pytest.raises(ValueError):
         c.append(0, k, k, i.long(), i[:1])
     with pytest.raises(ValueError):
         c.append(0, k, k, i, i[:1], q=k)
