@@ -5,25 +5,35 @@
 //
 // attend_general_kernel is fp32 arithmetic throughout: fp32 caches and queries
 // (which tensor-core products would round) and the head widths that the other
-// kernels do not take.  A block of 128 threads holds 32 flattened query rows,
-// four threads a row, and walks the keys 32 at a time through shared memory with
-// a running maximum and sum.  Bound by shared-memory reads: four FMA of scores
-// take a 16-byte read of keys.
+// kernels do not take.  A block of 128 threads holds 16 flattened query rows,
+// eight threads a row, and walks the keys 32 at a time, two to four blocks of them
+// on the way in shared memory, with a running maximum and sum.  Bound by
+// shared-memory reads: four FMA of scores take a 16-byte read of keys.
 #include <algorithm>
 #include <cmath>
 #include <string>
+#include <type_traits>
 
 #include "hf_attend.cuh"
 
 namespace hf {
 namespace {
 
-constexpr int kRows = 32, kKeys = 32, kThreads = 128;
+constexpr int kRows = 16, kKeys = 32, kThreads = 128;
+constexpr int kTeam = kThreads / kRows;  // threads of a row
 
-template <int D>
-constexpr size_t general_smem() {
-  return sizeof(float) * ((kRows + kKeys) * (D + 4) + kKeys * D + kRows * (kKeys + 1)) + sizeof(int) * kKeys;
-}
+// Shared memory: queries in fp32, two to four buffers of keys and values as the cache
+// holds them (expanded to fp32 from codes), the block's probabilities, and the
+// rows of the blocks to come.
+template <typename T, int KIND, int D>
+struct General {
+  using E = typename std::conditional<KIND == HF_CACHE_Q4, float, T>::type;  // keys and values in shared memory
+  static constexpr int kPitch = D + 16 / static_cast<int>(sizeof(E));
+  static constexpr int kBuffer = 2 * kKeys * kPitch;  // keys, then values
+  static constexpr int kBuffers = D <= 64 ? 4 : D <= 128 ? 3 : 2;
+  static constexpr size_t kBytes = sizeof(float) * (kRows * (D + 4) + kRows * (kKeys + 1)) +
+                                   kBuffers * (kBuffer * sizeof(E) + kKeys * sizeof(int));
+};
 
 // Eight channels of a row and head, chunk c, in fp32.
 template <typename T>
@@ -41,30 +51,36 @@ __device__ __forceinline__ void load_chunk(const T* p, float* x) {
     x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
   }
 }
-template <typename T, int KIND, int D>
-__device__ __forceinline__ void load_cache_chunk(const CacheArgs& C, bool value, int row, int h, int c, float* x) {
-  if constexpr (KIND == HF_CACHE_Q4) {
-    const int64_t at = static_cast<int64_t>(h) * C.rows + row;
-    const int g = c / 4, m = c % 4;
-    const uint16_t* codes = reinterpret_cast<const uint16_t*>((value ? C.v : C.k) + at * (D / 2)) + (D / 32) * 2 * m + g;
-    const uint16_t s16 = reinterpret_cast<const uint16_t*>((value ? C.vs : C.ks) + at * (D / 16))[g];
-    const float s = __uint_as_float(static_cast<uint32_t>(s16) << 16);
-    const uint32_t w = codes[0] | static_cast<uint32_t>(codes[D / 32]) << 16;
+template <int D>
+__device__ __forceinline__ void load_codes_chunk(const CacheArgs& C, bool value, int row, int h, int c, float* x) {
+  const int64_t at = static_cast<int64_t>(h) * C.rows + row;
+  const int g = c / 4, m = c % 4;
+  const uint16_t* codes = reinterpret_cast<const uint16_t*>((value ? C.v : C.k) + at * (D / 2)) + (D / 32) * 2 * m + g;
+  const uint16_t s16 = reinterpret_cast<const uint16_t*>((value ? C.vs : C.ks) + at * (D / 16))[g];
+  const float s = __uint_as_float(static_cast<uint32_t>(s16) << 16);
+  const uint32_t w = codes[0] | static_cast<uint32_t>(codes[D / 32]) << 16;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = s * static_cast<float>(static_cast<int>((w >> (4 * e)) & 15u) - 8);
-  } else {
-    load_chunk(reinterpret_cast<const T*>(value ? C.v : C.k) + row * C.row_stride + h * C.head_stride + 8 * c, x);
-  }
+  for (int e = 0; e < 8; ++e) x[e] = s * static_cast<float>(static_cast<int>((w >> (4 * e)) & 15u) - 8);
+}
+__device__ __forceinline__ float4 four(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 four(const __nv_bfloat16* p) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                     __uint_as_float(u.y & 0xffff0000u));
+}
+__device__ __forceinline__ void cp_async_16_or_zero(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
 template <typename T, int KIND, int D>
 __global__ void __launch_bounds__(kThreads) attend_general_kernel(const CacheArgs C, const AttendArgs A, int ns) {
-  extern __shared__ __align__(16) float smem_f[];
-  float* sQ = smem_f;
-  float* sK = sQ + kRows * (D + 4);
-  float* sV = sK + kKeys * (D + 4);
-  float* sP = sV + kKeys * D;
-  int* sRow = reinterpret_cast<int*>(sP + kRows * (kKeys + 1));
+  using L = General<T, KIND, D>;
+  using E = typename L::E;
+  extern __shared__ __align__(16) uint8_t smem_g[];
+  float* sQ = reinterpret_cast<float*>(smem_g);
+  float* sP = sQ + kRows * (D + 4);
+  E* sKV = reinterpret_cast<E*>(sP + kRows * (kKeys + 1));
+  int* sRow = reinterpret_cast<int*>(sKV + L::kBuffers * L::kBuffer);
   depend_wait();
   depend_launch();
   const TilePlace at = find_tile(C, A, kRows, blockIdx.x);
@@ -73,8 +89,45 @@ __global__ void __launch_bounds__(kThreads) attend_general_kernel(const CacheArg
   const int h = blockIdx.y, sp = blockIdx.z;
   const int r0 = at.at * kRows;
   const int n_rows = static_cast<int>(min(static_cast<int64_t>(kRows), static_cast<int64_t>(span.n) * A.G - r0));
-  const int r = threadIdx.x >> 2, c4 = threadIdx.x & 3;
+  const int r = threadIdx.x / kTeam, c4 = threadIdx.x % kTeam;
 
+  const int last = seen(span, A.causal, (r0 + n_rows - 1) / A.G);
+  const int per = ((last + ns - 1) / ns + kKeys - 1) / kKeys * kKeys;
+  const int k0 = static_cast<int>(min(static_cast<int64_t>(sp) * per, static_cast<int64_t>(last)));
+  const int k1 = static_cast<int>(min(static_cast<int64_t>(k0) + per, static_cast<int64_t>(last)));
+  const int mine = r < n_rows ? min(seen(span, A.causal, (r0 + r) / A.G), k1) : 0;
+
+  auto find_rows = [&](int kb, int buf) {  // of the block at key kb
+    if (threadIdx.x < kKeys) {
+      const int key = kb + threadIdx.x;
+      sRow[buf * kKeys + threadIdx.x] = key < k1 ? cache_row(C, at.seq, key) : -1;
+    }
+  };
+  auto bring = [&](int buf) {  // the block whose rows lie in sRow[buf]
+    E* dst = sKV + buf * L::kBuffer;
+    if constexpr (KIND == HF_CACHE_Q4) {
+      for (int i = threadIdx.x; i < 2 * kKeys * (D / 8); i += kThreads) {
+        const int key = i / (D / 8), c = i % (D / 8);  // keys, then values
+        const int row = sRow[buf * kKeys + key % kKeys];
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (row >= 0) load_codes_chunk<D>(C, key >= kKeys, row, h, c, x);
+        reinterpret_cast<float4*>(dst + key * L::kPitch + 8 * c)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        reinterpret_cast<float4*>(dst + key * L::kPitch + 8 * c)[1] = make_float4(x[4], x[5], x[6], x[7]);
+      }
+    } else {
+      constexpr int kPer = 16 / static_cast<int>(sizeof(E)), kChunks = D / kPer;
+      for (int i = threadIdx.x; i < 2 * kKeys * kChunks; i += kThreads) {
+        const int key = i / kChunks, c = i % kChunks;
+        const int row = sRow[buf * kKeys + key % kKeys];
+        const E* src = reinterpret_cast<const E*>(key >= kKeys ? C.v : C.k) + max(row, 0) * C.row_stride +
+                       h * C.head_stride + kPer * c;
+        cp_async_16_or_zero(smem_addr(dst + key * L::kPitch + kPer * c), src, row >= 0);
+      }
+    }
+  };
+  constexpr int kBuffers = L::kBuffers;
+#pragma unroll
+  for (int b = 0; b < kBuffers; ++b) find_rows(k0 + b * kKeys, b);
   for (int i = threadIdx.x; i < kRows * (D / 8); i += kThreads) {
     const int row = i / (D / 8), c = i % (D / 8);
     float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -86,80 +139,81 @@ __global__ void __launch_bounds__(kThreads) attend_general_kernel(const CacheArg
 #pragma unroll
     for (int e = 0; e < 8; ++e) sQ[row * (D + 4) + 8 * c + e] = x[e];
   }
-  const int last = seen(span, A.causal, (r0 + n_rows - 1) / A.G);
-  const int per = ((last + ns - 1) / ns + kKeys - 1) / kKeys * kKeys;
-  const int k0 = min(static_cast<int64_t>(sp) * per, static_cast<int64_t>(last));
-  const int k1 = min(static_cast<int64_t>(k0) + per, static_cast<int64_t>(last));
-  const int mine = r < n_rows ? min(seen(span, A.causal, (r0 + r) / A.G), k1) : 0;
+  __syncthreads();
+#pragma unroll
+  for (int b = 0; b < kBuffers - 1; ++b) {
+    if (k0 + b * kKeys < k1) bring(b);
+    cp_async_commit();
+  }
 
-  float acc[D / 4], m = -INFINITY, l = 0.f;
+  constexpr int kMine = D / kTeam;  // channels of a thread, by fours
+  float acc[kMine], m = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int i = 0; i < D / 4; ++i) acc[i] = 0.f;
-  for (int kb = k0; kb < k1; kb += kKeys) {
-    __syncthreads();
-    if (threadIdx.x < kKeys) sRow[threadIdx.x] = kb + threadIdx.x < k1 ? cache_row(C, at.seq, kb + threadIdx.x) : -1;
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * kKeys * (D / 8); i += kThreads) {
-      const bool value = i >= kKeys * (D / 8);
-      const int j = value ? i - kKeys * (D / 8) : i;
-      const int key = j / (D / 8), c = j % (D / 8);
-      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (sRow[key] >= 0) load_cache_chunk<T, KIND, D>(C, value, sRow[key], h, c, x);
-      float* dst = value ? sV + key * D + 8 * c : sK + key * (D + 4) + 8 * c;
-      reinterpret_cast<float4*>(dst)[0] = make_float4(x[0], x[1], x[2], x[3]);
-      reinterpret_cast<float4*>(dst)[1] = make_float4(x[4], x[5], x[6], x[7]);
-    }
-    __syncthreads();
-    float s[kKeys / 4];
+  for (int i = 0; i < kMine; ++i) acc[i] = 0.f;
+  int buf = 0;
+  for (int kb = k0; kb < k1; kb += kKeys, buf = buf + 1 == kBuffers ? 0 : buf + 1) {
+    cp_async_wait<kBuffers - 2>();
+    __syncthreads();  // this block is there, the one before it is read, the rows to come are known
+    if (kb + (kBuffers - 1) * kKeys < k1) bring(buf == 0 ? kBuffers - 1 : buf - 1);
+    cp_async_commit();
+    find_rows(kb + kBuffers * kKeys, buf);
+    const E* sK = sKV + buf * L::kBuffer;
+    const E* sV = sK + kKeys * L::kPitch;
+    float s[kKeys / kTeam];
 #pragma unroll
-    for (int i = 0; i < kKeys / 4; ++i) s[i] = 0.f;
-#pragma unroll 4
+    for (int i = 0; i < kKeys / kTeam; ++i) s[i] = 0.f;
+#pragma unroll 8
     for (int d = 0; d < D; d += 4) {
-      const float4 q = *reinterpret_cast<const float4*>(sQ + r * (D + 4) + d);
+      const float4 q = four(sQ + r * (D + 4) + d);
 #pragma unroll
-      for (int i = 0; i < kKeys / 4; ++i) {
-        const float4 k = *reinterpret_cast<const float4*>(sK + (c4 + 4 * i) * (D + 4) + d);
+      for (int i = 0; i < kKeys / kTeam; ++i) {
+        const float4 k = four(sK + (c4 + kTeam * i) * L::kPitch + d);
         s[i] = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, fmaf(q.w, k.w, s[i]))));
       }
     }
     float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kKeys / 4; ++i) {
-      s[i] = kb + c4 + 4 * i < mine ? s[i] * A.scale_log2 : -INFINITY;
-      // a NaN score has to stay one: it reaches the sum below
-      top = fmaxf(top, s[i]);
+    for (int i = 0; i < kKeys / kTeam; ++i) {
+      s[i] = kb + c4 + kTeam * i < mine ? s[i] * A.scale_log2 : -INFINITY;
+      top = fmaxf(top, s[i]);  // passes by a NaN, which reaches the sum below
     }
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+#pragma unroll
+    for (int o = 1; o < kTeam; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const float m_new = fmaxf(m, top);
     const float base = m_new == -INFINITY ? 0.f : m_new;
     const float fix = exp2f(m - base);
     m = m_new;
     l *= fix;
 #pragma unroll
-    for (int i = 0; i < D / 4; ++i) acc[i] *= fix;
+    for (int i = 0; i < kMine; ++i) acc[i] *= fix;
 #pragma unroll
-    for (int i = 0; i < kKeys / 4; ++i) {
+    for (int i = 0; i < kKeys / kTeam; ++i) {
       const float p = exp2f(s[i] - base);
       l += p;
-      sP[r * (kKeys + 1) + c4 + 4 * i] = p;
+      sP[r * (kKeys + 1) + c4 + kTeam * i] = p;
     }
     __syncwarp();
-    const int keys = min(kKeys, mine - kb);  // what this row does not see adds nothing, whatever it holds
-    for (int key = 0; key < keys; ++key) {
+    auto add = [&](int key) {
       const float p = sP[r * (kKeys + 1) + key];
 #pragma unroll
-      for (int j = 0; j < D / 16; ++j) {
-        const float4 v = *reinterpret_cast<const float4*>(sV + key * D + 16 * j + 4 * c4);
+      for (int j = 0; j < kMine / 4; ++j) {
+        const float4 v = four(sV + key * L::kPitch + 4 * kTeam * j + 4 * c4);
         acc[4 * j] = fmaf(p, v.x, acc[4 * j]);
         acc[4 * j + 1] = fmaf(p, v.y, acc[4 * j + 1]);
         acc[4 * j + 2] = fmaf(p, v.z, acc[4 * j + 2]);
         acc[4 * j + 3] = fmaf(p, v.w, acc[4 * j + 3]);
       }
+    };
+    if (__all_sync(0xffffffffu, mine - kb >= kKeys)) {
+#pragma unroll 8
+      for (int key = 0; key < kKeys; ++key) add(key);
+    } else {  // what a row does not see adds nothing, whatever it holds
+      for (int key = 0; key < mine - kb && key < kKeys; ++key) add(key);
     }
   }
-  l += __shfl_xor_sync(0xffffffffu, l, 1);
-  l += __shfl_xor_sync(0xffffffffu, l, 2);
+  cp_async_wait<0>();
+#pragma unroll
+  for (int o = 1; o < kTeam; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
   if (r >= n_rows) return;
   const int rr = r0 + r;
   const int64_t tok = span.first + rr / A.G;
@@ -167,8 +221,8 @@ __global__ void __launch_bounds__(kThreads) attend_general_kernel(const CacheArg
   if (ns > 1) {
     const int64_t slot = (static_cast<int64_t>(sp) * A.n_tok + tok) * A.H_q + hq;
 #pragma unroll
-    for (int j = 0; j < D / 16; ++j)
-      *reinterpret_cast<float4*>(A.part_o + slot * D + 16 * j + 4 * c4) =
+    for (int j = 0; j < kMine / 4; ++j)
+      *reinterpret_cast<float4*>(A.part_o + slot * D + 4 * kTeam * j + 4 * c4) =
           make_float4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
     if (c4 == 0) A.part_ml[slot] = make_float2(m, l);
     return;
@@ -176,9 +230,9 @@ __global__ void __launch_bounds__(kThreads) attend_general_kernel(const CacheArg
   T* dst = reinterpret_cast<T*>(A.out) + tok * A.o_row + hq * A.o_head;
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-  for (int j = 0; j < D / 16; ++j)
+  for (int j = 0; j < kMine / 4; ++j)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) dst[16 * j + 4 * c4 + e] = from_float<T>(acc[4 * j + e] * inv);
+    for (int e = 0; e < 4; ++e) dst[4 * kTeam * j + 4 * c4 + e] = from_float<T>(acc[4 * j + e] * inv);
   if (A.lse && c4 == 0) A.lse[tok * A.H_q + hq] = (m + log2f(l)) * 0.693147180559945309f;
 }
 
@@ -217,17 +271,18 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttendArgs A, in
 template <typename T, int KIND, int D>
 hf_status launch_general(const CacheArgs& c, const AttendArgs& a, int max_kv, cudaStream_t stream) {
   const int64_t tiles = most_tiles(a.n_tok, a.G, c.n_seq, kRows);
-  // keys are split where the tiles alone leave SMs idle, in parts of 128 keys at
-  // least, as far as the workspace goes
-  int64_t ns = std::min<int64_t>(2 * device_sm_count() / std::max<int64_t>(tiles * c.H, 1), (max_kv + 127) / 128);
+  // keys are split where the tiles alone leave SMs idle, in parts of 256 keys at
+  // least (joining them takes a launch), as far as the workspace goes
+  int64_t ns = std::min<int64_t>(2 * device_sm_count() / std::max<int64_t>(tiles * c.H, 1), (max_kv + 255) / 256);
   ns = std::min<int64_t>(ns, part_rows(device_sm_count()) / (static_cast<int64_t>(a.n_tok) * a.H_q));
   ns = std::max<int64_t>(1, std::min<int64_t>(ns, 64));
   auto kern = attend_general_kernel<T, KIND, D>;
+  constexpr size_t smem = General<T, KIND, D>::kBytes;
   HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                   static_cast<int>(general_smem<D>())),
+                                   static_cast<int>(smem)),
               "hf_attend: shared memory size");
   HF_CUDA_TRY(launch_dependent(kern, dim3(static_cast<unsigned>(tiles), c.H, static_cast<unsigned>(ns)), dim3(kThreads),
-                               general_smem<D>(), stream, c, a, static_cast<int>(ns)),
+                               smem, stream, c, a, static_cast<int>(ns)),
               "hf_attend: launch");
   if (ns > 1) return launch_join(sizeof(T) == 2 ? HF_BF16 : HF_F32, D, a, static_cast<int>(ns), stream);
   return HF_OK;
