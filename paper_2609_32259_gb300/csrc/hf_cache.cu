@@ -9,7 +9,7 @@
 // bits and codes rint(y / scale) + 8.
 //
 // Bound by HBM: every key, value and query is read once and written once.  A
-// warp takes one token (its sequence, row and position are found once), 4 lanes
+// warp takes one token at a time (its sequence, row and position are found once), 4 lanes
 // a head (2 where D / 16 is not a multiple of 4), each lane the 8-channel
 // chunks m, m + 4, ... of it: chunk c and its rotation partner c + D / 16 fall to
 // one lane, a 4-bit group is one chunk of each of the 4 lanes, and the codes of
@@ -115,20 +115,32 @@ struct Lanes {
   static constexpr int kChunks = D / 8 / kPerHead;     // 8-channel chunks a lane
 };
 
-// Eight channels.
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float* x) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// Eight channels as they lie in memory, and in fp32.
+template <typename T>
+struct Raw8 {
+  uint4 u[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_raw8(const T* p) {
+  Raw8<T> r;
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) r.u[i] = reinterpret_cast<const uint4*>(p)[i];
+  return r;
+}
+__device__ __forceinline__ void floats(const Raw8<__nv_bfloat16>& r, float* x) {
+  const uint32_t w[4] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[2 * i] = __uint_as_float(w[i] << 16);
     x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
   }
 }
-__device__ __forceinline__ void load8(const float* p, float* x) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+__device__ __forceinline__ void floats(const Raw8<float>& r, float* x) {
+  const uint32_t w[8] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w, r.u[1].x, r.u[1].y, r.u[1].z, r.u[1].w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
 }
+__device__ __forceinline__ void load8(const float* p, float* x) { floats(load_raw8(p), x); }
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x) {
   *reinterpret_cast<uint4*>(p) = pack16(x, static_cast<const __nv_bfloat16*>(nullptr));
 }
@@ -166,6 +178,34 @@ __device__ __forceinline__ void load_words(const void* p, uint32_t* w) {
   }
 }
 
+// Codes of eight values, four bits each: rint(y / s) + 8, the quotient rounded to
+// fp32, for |y| <= 7.25 s and inv = 1 / s.  y inv is within 2^-20 of the quotient,
+// so its integer c is the quotient's unless that lies as near to a half.  y - c s
+// says whether it does: an exact half goes to the even neighbour, and the few
+// others (*near) have to be divided.
+__device__ __forceinline__ uint32_t q4_codes(const float (&y)[8], float s, float inv, bool* near) {
+  const float kWhole = 12582912.f;  // 1.5 * 2^23: sums with it are rounded to integers
+  const float half = 0.5f * s, close = s * 7.62939453125e-6f;  // 2^-17
+  uint32_t w = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float t = __fmaf_rn(y[e], inv, kWhole);
+    const float r = __fmaf_rn(kWhole - t, s, y[e]), past = fabsf(r) - half;
+    uint32_t c = __float_as_uint(t) + 8u;
+    if (past == 0.f && (c & 1u)) c += r > 0.f ? 1u : ~0u;
+    *near |= past != 0.f && fabsf(past) <= close;
+    w |= (c & 15u) << (4 * e);
+  }
+  return w;
+}
+__device__ __noinline__ uint32_t q4_codes_divided(float y0, float y1, float y2, float y3, float y4, float y5, float y6,
+                                                  float y7, float s) {
+  const float y[8] = {y0, y1, y2, y3, y4, y5, y6, y7};
+  uint32_t w = 0;
+  for (int e = 0; e < 8; ++e) w |= static_cast<uint32_t>(static_cast<int>(rintf(__fdiv_rn(y[e], s))) + 8) << (4 * e);
+  return w;
+}
+
 // A head's channels x (this lane's chunks) as 4-bit codes and scales; called by
 // whole warps, for heads that are stored or not.
 template <int D>
@@ -186,12 +226,11 @@ __device__ __forceinline__ void store_q4(char* codes, char* scales, int m, bool 
     a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
     const float s = q4_scale(a);
     sc[g] = __float_as_uint(s) >> 16;
-    uint32_t w = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      // zero and NaN scales: every code is 8
-      const float c = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(x[g][e], s)), -7.f), 7.f) : 0.f;
-      w |= static_cast<uint32_t>(static_cast<int>(c) + 8) << (4 * e);
+    uint32_t w = 0x88888888u;  // zero and NaN scales: every code is 8
+    if (s > 0.f) {
+      bool near = false;
+      w = q4_codes(x[g], s, __frcp_rn(s), &near);
+      if (near) w = q4_codes_divided(x[g][0], x[g][1], x[g][2], x[g][3], x[g][4], x[g][5], x[g][6], x[g][7], s);
     }
     half[g] = w & 0xffffu;       // channels 4 j .. + 3 of the group, j = 2 m
     half[NG + g] = w >> 16;      // j = 2 m + 1
@@ -209,164 +248,275 @@ __device__ __forceinline__ void store_q4(char* codes, char* scales, int m, bool 
   }
 }
 
+// Where a packed token belongs, found by a whole warp; up to 32 sequences lie in
+// the lanes' registers.
+struct Places {
+  int end, first, start, pos0;
+  __device__ __forceinline__ Places(const CacheArgs& C, const TokenArgs& t, const int32_t* d_pos0) {
+    const int lane = threadIdx.x & 31;
+    end = 0x7fffffff, first = start = pos0 = 0;
+    if (lane < C.n_seq) {
+      first = t.tok_ptr[lane];
+      end = t.tok_ptr[lane + 1];
+      start = t.start[lane];
+      pos0 = d_pos0 ? d_pos0[lane] : 0;
+    }
+  }
+  // The cache row of token `tok`, and its position (by how much rows and
+  // positions differ: d_pos0); -1 and a status bit where there is none.
+  __device__ __forceinline__ int row(const CacheArgs& C, const TokenArgs& t, const int32_t* d_pos0, int tok,
+                                     int64_t* pos) const {
+    int seq, f, s, p;
+    if (C.n_seq <= 32) {
+      seq = __popc(__ballot_sync(0xffffffffu, end <= tok));
+      f = __shfl_sync(0xffffffffu, first, seq & 31);
+      s = __shfl_sync(0xffffffffu, start, seq & 31);
+      p = __shfl_sync(0xffffffffu, pos0, seq & 31);
+    } else {
+      seq = sequence_of(t.tok_ptr, C.n_seq, tok);
+      const int at = min(seq, C.n_seq - 1);
+      f = t.tok_ptr[at], s = t.start[at], p = d_pos0 ? d_pos0[at] : 0;
+    }
+    if (seq >= C.n_seq || f > tok || f < 0) {
+      set_status(C, HF_CHECK_BAD_OFFSETS);
+      return -1;
+    }
+    const int64_t r = static_cast<int64_t>(s) + (tok - f);
+    *pos = r + p;
+    if (r < 0) {
+      set_status(C, HF_CHECK_CAPACITY);
+      return -1;
+    }
+    return cache_row(C, seq, r);
+  }
+};
+
+// A warp goes from token to token (and through a token's heads, values first:
+// they need no rotation), always with the channels of the next kAhead steps on the
+// way to shared memory, each lane's for itself, the next tokens' among them: what
+// a token needs before its first channel, a chain of loads, would otherwise take
+// longer than the rest.
+constexpr int kAhead = 2;
+template <typename T, int D>
+constexpr int kRingWords = (kAhead + 1) * Lanes<D>::kChunks * static_cast<int>(sizeof(T)) / 2 * 32;  // uint4 a warp
+
 template <typename T, int KIND, int D>
-__global__ void __launch_bounds__(32 * kWarps) append_kernel(const CacheArgs C, const AppendArgs A) {
-  using L = Lanes<D>;
-  constexpr int NC = L::kChunks;
+__global__ void __launch_bounds__(32 * kWarps, D <= 128 ? 4 : 1) append_kernel(const CacheArgs C, const AppendArgs A) {
   depend_wait();
   depend_launch();
-  const int lane = threadIdx.x & 31;
-  const int tok = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  using L = Lanes<D>;
+  constexpr int NC = L::kChunks;
+  const int lane = threadIdx.x & 31, m = lane % L::kPerHead;
+  const int n_heads = 2 * C.H + A.H_q, step = gridDim.y * L::kHeads, h_first = blockIdx.y * L::kHeads;
+  const int stride = gridDim.x * kWarps;
+  int tok = blockIdx.x * kWarps + (threadIdx.x >> 5);
   if (tok >= A.t.n_tok) return;
-  const int seq = sequence_of(A.t.tok_ptr, C.n_seq, tok);
-  const int first = seq < C.n_seq ? A.t.tok_ptr[seq] : 0;
-  if (seq >= C.n_seq || first > tok || first < 0) {
-    if (lane == 0) set_status(C, HF_CHECK_BAD_OFFSETS);
-    return;
-  }
-  const int64_t t = static_cast<int64_t>(A.t.start[seq]) + (tok - first);
-  const int64_t pos = t + (A.pos0 ? A.pos0[seq] : 0);
-  if (t < 0 || (A.rope && (pos < 0 || pos >= A.rope_len))) {
-    if (lane == 0) set_status(C, HF_CHECK_CAPACITY);
-    return;
-  }
-  const int row = cache_row(C, seq, t);
-  if (row < 0) return;
-  const float* rope = A.rope ? A.rope + pos * D : nullptr;
-
-  const int m = lane % L::kPerHead;
-  const int n_heads = 2 * C.H + A.H_q;
-  for (int h0 = blockIdx.y * L::kHeads; h0 < n_heads; h0 += gridDim.y * L::kHeads) {
-    const int hh = h0 + lane / L::kPerHead;
-    const bool live = hh < n_heads;
-    const int role = hh < C.H ? 0 : hh < 2 * C.H ? 1 : 2;  // key, value, query
-    const int h = role == 0 ? hh : role == 1 ? hh - C.H : hh - 2 * C.H;
-    float x[NC][8];
-    const T* src = role == 0   ? reinterpret_cast<const T*>(A.k) + tok * A.k_row + h * A.k_head
-                   : role == 1 ? reinterpret_cast<const T*>(A.v) + tok * A.v_row + h * A.v_head
-                               : reinterpret_cast<const T*>(A.q) + tok * A.q_row + h * A.q_head;
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-      if (live) {
-        load8(src + 8 * (m + L::kPerHead * i), x[i]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
-      }
-    }
-    const float* g = role == 0 ? A.k_norm : role == 2 ? A.q_norm : nullptr;
-    if (A.k_norm || A.q_norm) {
-      float sum = 0.f;
+  const Places places(C, A.t, A.pos0);
+  int64_t pos = 0, next_pos = 0;
+  int row = places.row(C, A.t, A.pos0, tok, &pos), next_row = -1;
+  extern __shared__ __align__(16) uint4 ring[];
+  constexpr int kPer = sizeof(T) / 2;  // 16-byte words of a chunk
+  uint4* mine = ring + (threadIdx.x >> 5) * kRingWords<T, D> + lane;
+  int f_tok = tok, f_h = h_first, f_stage = 0;  // what is fetched next, and where to
+  auto fetch = [&]() {
+    const int hh = f_h + lane / L::kPerHead;
+    if (f_tok < A.t.n_tok && hh < n_heads) {
+      const T* src = hh < C.H       ? reinterpret_cast<const T*>(A.v) + f_tok * A.v_row + hh * A.v_head
+                     : hh < 2 * C.H ? reinterpret_cast<const T*>(A.k) + f_tok * A.k_row + (hh - C.H) * A.k_head
+                                    : reinterpret_cast<const T*>(A.q) + f_tok * A.q_row + (hh - 2 * C.H) * A.q_head;
+      uint4* dst = mine + f_stage * (NC * kPer * 32);
 #pragma unroll
       for (int i = 0; i < NC; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fmaf(x[i][e], x[i][e], sum);
-#pragma unroll
-      for (int o = 1; o < L::kPerHead; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      if (g) {
-        const float r = 1.f / sqrtf(sum / D + A.eps);
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-          float w[8];
-          load8(g + 8 * (m + L::kPerHead * i), w);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[i][e] = x[i][e] * r * w[e];
-        }
-      }
+        for (int e = 0; e < kPer; ++e)
+          cp_async_16(smem_addr(dst + (i * kPer + e) * 32),
+                      reinterpret_cast<const uint4*>(src + 8 * (m + L::kPerHead * i)) + e);
     }
-    if (rope && role != 1) {
+    cp_async_commit();
+    if ((f_h += step) >= n_heads) {
+      f_h = h_first;
+      f_tok = static_cast<int>(min(static_cast<int64_t>(f_tok) + stride, static_cast<int64_t>(A.t.n_tok)));
+    }
+    if (++f_stage == kAhead + 1) f_stage = 0;
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) fetch();
+  int stage = 0;
+  for (; tok < A.t.n_tok; tok += stride, row = next_row, pos = next_pos) {
+    if (row >= 0 && A.rope && (pos < 0 || pos >= A.rope_len)) {
+      set_status(C, HF_CHECK_CAPACITY);
+      row = -1;
+    }
+    float co[NC / 2][8], si[NC / 2][8];  // of this lane's pairs: the same for every head
+    if (A.rope && row >= 0) {
+      const float* rope = A.rope + pos * D;
 #pragma unroll
       for (int i = 0; i < NC / 2; ++i) {
         float cs[16];
         load8(rope + 16 * (m + L::kPerHead * i), cs);
         load8(rope + 16 * (m + L::kPerHead * i) + 8, cs + 8);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          // rounded one by one: 4-bit codes must not hang on what is contracted
-          const float a = x[i][e], b = x[i + NC / 2][e], c = cs[2 * e], s = cs[2 * e + 1];
-          x[i][e] = __fsub_rn(__fmul_rn(a, c), __fmul_rn(b, s));
-          x[i + NC / 2][e] = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
-        }
+        for (int e = 0; e < 8; ++e) co[i][e] = cs[2 * e], si[i][e] = cs[2 * e + 1];
       }
     }
-    if constexpr (KIND == HF_CACHE_Q4) {
-      if (h0 < 2 * C.H) {  // all lanes join the groups' maxima
-        const int64_t at = static_cast<int64_t>(role < 2 ? h : 0) * C.rows + row;
-        store_q4<D>((role == 1 ? C.v : C.k) + at * (D / 2), (role == 1 ? C.vs : C.ks) + at * (D / 16), m,
-                    live && role < 2, x);
+    next_row = tok + stride < A.t.n_tok ? places.row(C, A.t, A.pos0, tok + stride, &next_pos) : -1;
+    for (int h0 = h_first; h0 < n_heads; h0 += step) {
+      const int hh = h0 + lane / L::kPerHead;
+      const bool live = hh < n_heads;
+      const int role = hh < C.H ? 1 : hh < 2 * C.H ? 0 : 2;  // value, key, query
+      const int h = role == 1 ? hh : role == 0 ? hh - C.H : hh - 2 * C.H;
+      float x[NC][8];
+      cp_async_wait<kAhead - 1>();
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        Raw8<T> raw;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) raw.u[e] = live ? mine[stage * (NC * kPer * 32) + (i * kPer + e) * 32] : uint4{};
+        floats(raw, x[i]);
       }
-    } else {
-      if (live && role < 2) {
-        T* dst = reinterpret_cast<T*>(role == 1 ? C.v : C.k) + row * C.row_stride + h * C.head_stride;
+      fetch();
+      if (++stage == kAhead + 1) stage = 0;
+      if (row < 0) continue;
+      const float* g = role == 0 ? A.k_norm : role == 2 ? A.q_norm : nullptr;
+      if (A.k_norm || A.q_norm) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum = fmaf(x[i][e], x[i][e], sum);
+#pragma unroll
+        for (int o = 1; o < L::kPerHead; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (g) {
+          const float r = 1.f / sqrtf(sum / D + A.eps);
+#pragma unroll
+          for (int i = 0; i < NC; ++i) {
+            float w[8];
+            load8(g + 8 * (m + L::kPerHead * i), w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] = x[i][e] * r * w[e];
+          }
+        }
+      }
+      if (A.rope && role != 1) {
+        // two channels an instruction, every product and sum rounded by itself:
+        // 4-bit codes must not hang on what is contracted
+        const uint64_t minus = pack2(-1.f, -1.f);
+#pragma unroll
+        for (int i = 0; i < NC / 2; ++i) {
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const uint64_t a = pack2(x[i][e], x[i][e + 1]), b = pack2(x[i + NC / 2][e], x[i + NC / 2][e + 1]);
+            const uint64_t c = pack2(co[i][e], co[i][e + 1]), s = pack2(si[i][e], si[i][e + 1]);
+            unpack2(fma2(mul2(b, s), minus, mul2(a, c)), &x[i][e], &x[i][e + 1]);
+            unpack2(add2(mul2(b, c), mul2(a, s)), &x[i + NC / 2][e], &x[i + NC / 2][e + 1]);
+          }
+        }
+      }
+      if constexpr (KIND == HF_CACHE_Q4) {
+        if (h0 < 2 * C.H) {  // all lanes join the groups' maxima
+          const int64_t at = static_cast<int64_t>(role < 2 ? h : 0) * C.rows + row;
+          store_q4<D>((role == 1 ? C.v : C.k) + at * (D / 2), (role == 1 ? C.vs : C.ks) + at * (D / 16), m,
+                      live && role < 2, x);
+        }
+      } else {
+        if (live && role < 2) {
+          T* dst = reinterpret_cast<T*>(role == 1 ? C.v : C.k) + row * C.row_stride + h * C.head_stride;
+#pragma unroll
+          for (int i = 0; i < NC; ++i) store8(dst + 8 * (m + L::kPerHead * i), x[i]);
+        }
+      }
+      if (live && role == 2) {
+        T* dst = reinterpret_cast<T*>(A.q_out) + tok * A.q_row + h * A.q_head;
 #pragma unroll
         for (int i = 0; i < NC; ++i) store8(dst + 8 * (m + L::kPerHead * i), x[i]);
       }
     }
-    if (live && role == 2) {
-      T* dst = reinterpret_cast<T*>(A.q_out) + tok * A.q_row + h * A.q_head;
-#pragma unroll
-      for (int i = 0; i < NC; ++i) store8(dst + 8 * (m + L::kPerHead * i), x[i]);
-    }
   }
 }
 
+// A lane's part of a head-row as the cache holds it.
+template <typename T, int KIND, int D>
+struct Held {
+  Raw8<T> raw[Lanes<D>::kChunks];
+};
+template <typename T, int D>
+struct Held<T, HF_CACHE_Q4, D> {
+  uint32_t w[D / 32], s[D / 64];
+};
+
 template <typename T, int KIND, int D>
 __global__ void __launch_bounds__(32 * kWarps) read_kernel(const CacheArgs C, const ReadArgs A) {
-  using L = Lanes<D>;
-  constexpr int NC = L::kChunks;
   depend_wait();
   depend_launch();
-  const int lane = threadIdx.x & 31;
-  const int tok = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  using L = Lanes<D>;
+  constexpr int NC = L::kChunks;
+  const int lane = threadIdx.x & 31, m = lane % L::kPerHead;
+  const int n_heads = 2 * C.H, step = gridDim.y * L::kHeads, h_first = blockIdx.y * L::kHeads;
+  const int stride = gridDim.x * kWarps;
+  int tok = blockIdx.x * kWarps + (threadIdx.x >> 5);
   if (tok >= A.t.n_tok) return;
-  const int seq = sequence_of(A.t.tok_ptr, C.n_seq, tok);
-  const int first = seq < C.n_seq ? A.t.tok_ptr[seq] : 0;
-  if (seq >= C.n_seq || first > tok || first < 0) {
-    if (lane == 0) set_status(C, HF_CHECK_BAD_OFFSETS);
-    return;
-  }
-  const int64_t t = static_cast<int64_t>(A.t.start[seq]) + (tok - first);
-  if (t < 0 && lane == 0) set_status(C, HF_CHECK_CAPACITY);
-  const int row = t < 0 ? -1 : cache_row(C, seq, t);
-  const int m = lane % L::kPerHead;
-  for (int h0 = blockIdx.y * L::kHeads; h0 < 2 * C.H; h0 += gridDim.y * L::kHeads) {
+  const Places places(C, A.t, nullptr);
+  int64_t pos;
+  int row = places.row(C, A.t, nullptr, tok, &pos), next_row = -1;
+  Held<T, KIND, D> held;
+  auto fetch = [&](int r, int h0) {  // this lane's part of row r, heads h0 ..
     const int hh = h0 + lane / L::kPerHead;
-    if (hh >= 2 * C.H) break;
     const bool val = hh >= C.H;
     const int h = val ? hh - C.H : hh;
-    float x[NC][8];
-    if (row < 0) {
+    if (r >= 0 && hh < n_heads) {
+      if constexpr (KIND == HF_CACHE_Q4) {
+        const int64_t at = static_cast<int64_t>(h) * C.rows + r;
+        load_words<D / 32>((val ? C.v : C.k) + at * (D / 2) + m * (D / 8), held.w);
+        load_words<D / 64>((val ? C.vs : C.ks) + at * (D / 16), held.s);
+      } else {
+        const T* src = reinterpret_cast<const T*>(val ? C.v : C.k) + r * C.row_stride + h * C.head_stride;
 #pragma unroll
-      for (int i = 0; i < NC; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
-    } else if constexpr (KIND == HF_CACHE_Q4) {
-      constexpr int NG = D / 32;
-      const int64_t at = static_cast<int64_t>(h) * C.rows + row;
-      uint32_t w[NG], s2[NG / 2];
-      load_words<NG>((val ? C.v : C.k) + at * (D / 2) + m * (D / 8), w);
-      load_words<NG / 2>((val ? C.vs : C.ks) + at * (D / 16), s2);
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        const float s = __uint_as_float(g & 1 ? s2[g / 2] & 0xffff0000u : s2[g / 2] << 16);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int i = j * NG + g;  // halfword
-          const uint32_t half = w[i / 2] >> (16 * (i & 1));
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            x[g][4 * j + e] = s * static_cast<float>(static_cast<int>((half >> (4 * e)) & 15u) - 8);
-        }
+        for (int i = 0; i < NC; ++i) held.raw[i] = load_raw8(src + 8 * (m + L::kPerHead * i));
       }
     } else {
-      const T* src = reinterpret_cast<const T*>(val ? C.v : C.k) + row * C.row_stride + h * C.head_stride;
-#pragma unroll
-      for (int i = 0; i < NC; ++i) load8(src + 8 * (m + L::kPerHead * i), x[i]);
+      held = Held<T, KIND, D>{};
     }
-    T* dst = val ? reinterpret_cast<T*>(A.v) + tok * A.v_row + h * A.v_head
-                 : reinterpret_cast<T*>(A.k) + tok * A.k_row + h * A.k_head;
+  };
+  fetch(row, h_first);
+  for (; tok < A.t.n_tok; tok += stride, row = next_row) {
+    next_row = tok + stride < A.t.n_tok ? places.row(C, A.t, nullptr, tok + stride, &pos) : -1;
+    for (int h0 = h_first; h0 < n_heads; h0 += step) {
+      const int hh = h0 + lane / L::kPerHead;
+      const bool val = hh >= C.H;
+      const int h = val ? hh - C.H : hh;
+      const Held<T, KIND, D> now = held;
+      if (h0 + step < n_heads)
+        fetch(row, h0 + step);
+      else
+        fetch(next_row, h_first);
+      if (hh >= n_heads) continue;
+      T* dst = val ? reinterpret_cast<T*>(A.v) + tok * A.v_row + h * A.v_head
+                   : reinterpret_cast<T*>(A.k) + tok * A.k_row + h * A.k_head;
+      if constexpr (KIND == HF_CACHE_Q4) {
+        constexpr int NG = D / 32;
 #pragma unroll
-    for (int i = 0; i < NC; ++i) store8(dst + 8 * (m + L::kPerHead * i), x[i]);
+        for (int g = 0; g < NG; ++g) {
+          const float s = __uint_as_float(g & 1 ? now.s[g / 2] & 0xffff0000u : now.s[g / 2] << 16);
+          float x[8];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int i = j * NG + g;  // halfword
+            const uint32_t half = now.w[i / 2] >> (16 * (i & 1));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              x[4 * j + e] = s * static_cast<float>(static_cast<int>((half >> (4 * e)) & 15u) - 8);
+          }
+          store8(dst + 8 * (m + 4 * g), x);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+          float x[8];
+          floats(now.raw[i], x);
+          store8(dst + 8 * (m + L::kPerHead * i), x);
+        }
+      }
+    }
   }
 }
 
@@ -384,27 +534,40 @@ __global__ void rope_table_kernel(const InvFreq inv, int half, int pos0, int64_t
   out[i] = make_float2(c, s);
 }
 
-// Warps of a token where there are few tokens: its heads' steps are shared out
-// until every SM has some 16 warps.
+// Blocks that fit the SMs at once, a token a warp or fewer; where that is fewer
+// than kRounds tokens a warp, their heads' steps are shared out too.
+constexpr int kRounds = 6;
 template <int D>
-dim3 token_grid(int n_tok, int heads) {
-  const int blocks = (n_tok + kWarps - 1) / kWarps;
+hf_status token_grid(const void* kern, size_t smem, int n_tok, int heads, dim3* grid) {
+  int per_sm = 1;
+  HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)),
+              "shared memory size");
+  HF_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, 32 * kWarps, smem), "occupancy");
+  const int blocks = (n_tok + kWarps - 1) / kWarps, most = std::max(1, per_sm) * device_sm_count();
   const int steps = (heads + Lanes<D>::kHeads - 1) / Lanes<D>::kHeads;
-  const int want = (device_sm_count() * 16 / kWarps + blocks - 1) / blocks;
-  return dim3(blocks, std::max(1, std::min(steps, want)));
+  const int want = (kRounds * most + blocks - 1) / blocks;
+  const int y = std::max(1, std::min(steps, want));
+  *grid = dim3(std::max(1, std::min(blocks, most / y)), y);
+  return HF_OK;
 }
 
 template <typename T, int KIND, int D>
 hf_status launch_append(const CacheArgs& c, const AppendArgs& a, cudaStream_t stream) {
-  HF_CUDA_TRY(launch_dependent(append_kernel<T, KIND, D>, token_grid<D>(a.t.n_tok, 2 * c.H + a.H_q), dim3(32 * kWarps),
-                               0, stream, c, a),
+  dim3 grid;
+  constexpr size_t smem = sizeof(uint4) * kWarps * kRingWords<T, D>;
+  const hf_status st =
+      token_grid<D>(reinterpret_cast<const void*>(append_kernel<T, KIND, D>), smem, a.t.n_tok, 2 * c.H + a.H_q, &grid);
+  if (st != HF_OK) return st;
+  HF_CUDA_TRY(launch_dependent(append_kernel<T, KIND, D>, grid, dim3(32 * kWarps), smem, stream, c, a),
               "hf_cache_append: launch");
   return HF_OK;
 }
 template <typename T, int KIND, int D>
 hf_status launch_read(const CacheArgs& c, const ReadArgs& a, cudaStream_t stream) {
-  HF_CUDA_TRY(launch_dependent(read_kernel<T, KIND, D>, token_grid<D>(a.t.n_tok, 2 * c.H), dim3(32 * kWarps), 0, stream,
-                               c, a),
+  dim3 grid;
+  const hf_status st = token_grid<D>(reinterpret_cast<const void*>(read_kernel<T, KIND, D>), 0, a.t.n_tok, 2 * c.H, &grid);
+  if (st != HF_OK) return st;
+  HF_CUDA_TRY(launch_dependent(read_kernel<T, KIND, D>, grid, dim3(32 * kWarps), 0, stream, c, a),
               "hf_cache_read: launch");
   return HF_OK;
 }
