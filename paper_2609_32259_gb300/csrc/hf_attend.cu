@@ -310,7 +310,8 @@ hf_status attend_general(const CacheArgs& c, const AttendArgs& a, hf_cache_kind 
 }
 
 size_t workspace_bytes_for(int D) {
-  return HF_ATTEND_ZEROED + static_cast<size_t>(part_rows(device_sm_count())) * (D + 2) * sizeof(float);
+  return HF_ATTEND_ZEROED + static_cast<size_t>(part_rows(device_sm_count())) * (D + 2) * sizeof(float) +
+         attend_cuts_bytes();
 }
 
 }  // namespace
@@ -381,12 +382,13 @@ extern "C" hf_status hf_attend(const hf_cache* cache, const hf_attend_desc* d, v
   a.zeroed = reinterpret_cast<int32_t*>(ws);
   a.part_o = reinterpret_cast<float*>(ws + HF_ATTEND_ZEROED);
   a.part_ml = reinterpret_cast<float2*>(a.part_o + part_rows(device_sm_count()) * c.D);
+  a.cuts = a.part_ml + part_rows(device_sm_count());
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
   const int max_kv = static_cast<int>(std::min<int64_t>(d->max_kv_len, c.rows));
   const int64_t max_rows = static_cast<int64_t>(std::min(d->max_q_len, d->n_tok)) * a.G;
   if (attend_rows_takes(cache->kind, d->dtype, c.D) && max_rows <= 16)
     return attend_rows(c, a, cache->kind, static_cast<int>(max_rows), stream);
-  if (attend_tiles_takes(cache->kind, d->dtype, c.D)) return attend_tiles(c, a, cache->kind, stream);
+  if (attend_tiles_takes(cache->kind, d->dtype, c.D)) return attend_tiles(c, a, cache->kind, max_kv, stream);
   switch (c.D) {
     case 32: return attend_general<32>(c, a, cache->kind, d->dtype, max_kv, stream);
     case 64: return attend_general<64>(c, a, cache->kind, d->dtype, max_kv, stream);

@@ -26,6 +26,7 @@ struct AttendArgs {
   float scale_log2;  // scale * log2(e)
   float* part_o;     // partial outputs [part rows][D]
   float2* part_ml;   // their m and l
+  void* cuts;        // units in several pieces
   int32_t* zeroed;   // counters, zero between calls
 };
 
@@ -136,7 +137,9 @@ hf_status attend_rows(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kin
 
 // The form for many query rows (hf_attend_tiles.cu): the same types and widths.
 bool attend_tiles_takes(hf_cache_kind kind, hf_dtype dtype, int D);
-hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, cudaStream_t stream);
+// max_kv: where it is short, sequences are not split.
+hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_kv, cudaStream_t stream);
+size_t attend_cuts_bytes();  // of AttendArgs::cuts
 
 // Joins `ns` parts of every (token, query head), [part][token][head].
 hf_status launch_join(hf_dtype dtype, int D, const AttendArgs& a, int ns, cudaStream_t stream);

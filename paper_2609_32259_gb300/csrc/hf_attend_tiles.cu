@@ -8,8 +8,8 @@
 // one's softmax runs under the other's products.  With at most 128 rows both tiles
 // are the same rows and take every other step.  One block an SM stays for the
 // whole call: the units' costs are shared out evenly, so long prompts end
-// together and the keys of a few short questions are split over all SMs; a
-// unit's pieces are joined by the last block at it.
+// together and the keys of a few short questions are split over all SMs; units
+// that were cut are joined by a kernel that follows.
 //
 //   warps 0-3, 4-7  queries and softmax of tile 0 and 1: a thread a row.  Scores come from
 //                   tensor memory, probabilities go back there as bf16 over them,
@@ -208,22 +208,23 @@ __device__ __forceinline__ void load_q4(Q4Words<D>& q, const char* codes, const 
     q.s[0] = *reinterpret_cast<const uint32_t*>(scales + r * 4);
   }
 }
-// Their values as bf16, exactly, into row `key` of the operand at `base`: 128 + c
-// by masking, - 136, times the scale, two codes at a time.
+// Their values as bf16, exactly, into row `key` of the operand at `base`: the bits
+// of c in the mantissa of 16 make 16 + c, and (16 + c) s - 24 s is (c - 8) s in one
+// operation for two codes (24 s has at most 7 significant bits).
 template <int D>
 __device__ __forceinline__ void store_q4_values(const Q4Words<D>& q, uint32_t base, int part, int key, int m) {
   constexpr int NG = D / 32;
-  const __nv_bfloat162 off = __floats2bfloat162_rn(136.f, 136.f);
+  const __nv_bfloat162 off = __floats2bfloat162_rn(-24.f, -24.f);
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     const uint32_t w = __byte_perm(q.w[g / 2], q.w[NG / 2 + g / 2], g & 1 ? 0x7632 : 0x5410);
     const uint32_t s2 = __byte_perm(q.s[g / 2], q.s[g / 2], g & 1 ? 0x3232 : 0x1010);
+    const __nv_bfloat162 s = *reinterpret_cast<const __nv_bfloat162*>(&s2), s24 = __hmul2(s, off);
     uint32_t v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t c = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;
-      const __nv_bfloat162 x =
-          __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&c), off), *reinterpret_cast<const __nv_bfloat162*>(&s2));
+      const uint32_t c = ((i == 0 ? w << 3 : w >> (4 * i - 3)) & 0x00780078u) | 0x41804180u;
+      const __nv_bfloat162 x = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&c), s, s24);
       v[i] = *reinterpret_cast<const uint32_t*>(&x);
     }
     const int c = 4 * g + m;
@@ -265,11 +266,20 @@ struct Piece {
   int32_t kv_end;
   int32_t dual;                  // at most 128 rows: both tiles are the same rows, and take the steps in turn
   // complete when the next piece is announced:
-  int32_t n_pieces;              // of the unit, in blocks c0 .. c1
-  int32_t c0, c1;
-  int32_t slot, slot0;           // of this piece, and of block c0's
+  int32_t n_pieces;              // of its unit
+  int32_t slot;                  // of its partial results
 };
 
+// A unit in several pieces, for the kernel that joins them: written by the block
+// with its first piece, which can have no second such unit (n_rows 0: it has
+// none).
+struct Cut {
+  int32_t n_rows, first, r0, h;
+  int32_t c0, blocks, slot0;       // blocks c0 .. c0 + blocks - 1, the slot of c0's piece
+  uint32_t mask[kMaxBlocks / 32];  // blocks c0 + i that have a piece
+};
+
+constexpr int kOwnSteps = 4;  // what starting and ending a unit takes, in steps
 struct UnitCost {
   int64_t w0, dw, head;  // cost of unit 0, its growth, all units of one head
   int tiles;
@@ -279,19 +289,22 @@ __device__ __forceinline__ UnitCost unit_cost(const SeqSpan& s, const AttendArgs
   const int64_t rows = static_cast<int64_t>(s.n) * A.G;
   u.tiles = static_cast<int>((rows + 2 * kTile - 1) / (2 * kTile));
   u.dw = A.causal ? 2 * kTile : 0;
-  u.w0 = (A.causal ? max(s.kv - s.n, 0) : s.kv) * static_cast<int64_t>(A.G) + u.dw + 2 * kTile * A.G;
+  u.w0 = (A.causal ? max(s.kv - s.n, 0) : s.kv) * static_cast<int64_t>(A.G) + u.dw + kOwnSteps * kTile * A.G;
   u.head = u.tiles * u.w0 + u.dw * (static_cast<int64_t>(u.tiles) * (u.tiles - 1) / 2);
   return u;
 }
 
 // Cuts of a unit with cost [w0, w0 + w) and n steps: the step where cost x lies.
-// A piece of less than two steps goes to its neighbour.
-__device__ __forceinline__ int cut(int64_t x, int64_t w0, int64_t w, int n) {
+// A piece of less than kLeastSteps goes to its neighbour; without `split` units
+// stay whole.
+constexpr int kLeastSteps = 6;
+__device__ __forceinline__ int cut(int64_t x, int64_t w0, int64_t w, int n, int split) {
   if (x <= w0) return 0;
   if (x >= w0 + w) return n;
   // fp32, rounded the same way by every block: it has to grow with x and no more
   const int p = static_cast<int>(static_cast<float>(x - w0) / static_cast<float>(w) * n);
-  return p < 2 ? 0 : p > n - 2 ? n : p;
+  if (!split) return 2 * p < n ? 0 : n;
+  return p < kLeastSteps ? 0 : p > n - kLeastSteps ? n : p;
 }
 template <int SRC, int D>
 struct Smem {
@@ -311,17 +324,15 @@ struct Shared {
   uint64_t q_full[2], s_full[2], p_full[2][2], o_full[2], turn[2];
   uint64_t piece_full[2], piece_empty[2];
   uint64_t drain, aux, meet;
-  float2 ml[2 * kTile];
+  float2 ml[kTile];
   Piece piece[2];
-  uint32_t mask[2][kMaxBlocks / 32];  // blocks c0 + i that have a piece of its unit
   uint32_t tmem;
-  int32_t last;
 };
 
 template <int SRC, int D>
 __global__ void __launch_bounds__(kThreads, 1)
     attend_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                        const CacheArgs C, const AttendArgs A, int box) {
+                        const CacheArgs C, const AttendArgs A, int box, int split) {
   using M = Smem<SRC, D>;
   constexpr int S = M::kStages;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -639,90 +650,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!meet()) break;
         tc_fence_after_sync();
       }
-      if (pc.n_pieces > 1) {
-        // the last block at the unit joins its pieces, in the blocks' order
-        if (!meet()) break;
-        if (threadIdx.x == 0) {
-          __threadfence();
-          sh.last = atomicAdd(A.zeroed + pc.c0, 1) == pc.n_pieces - 1;
-          if (sh.last) {
-            A.zeroed[pc.c0] = 0;
-            __threadfence();
-          }
-        }
-        if (!meet()) break;
-        if (sh.last) {
-          const int blocks = pc.c1 - pc.c0 + 1;
-          auto has = [&](int b) { return sh.mask[k & 1][b >> 5] >> (b & 31) & 1; };
-          auto row_at = [&](int b) { return static_cast<int64_t>(b ? 2 * (pc.c0 + b) : pc.slot0) * (2 * kTile); };
-          if (static_cast<int>(threadIdx.x) < n_rows) {  // a row's maximum and sum
-            const int q = threadIdx.x;
-            float top = -INFINITY;
-#pragma unroll 4
-            for (int b = 0; b < blocks; ++b)
-              if (has(b)) top = fmaxf(top, __ldcg(&A.part_ml[row_at(b) + q]).x);
-            const float zero = top == -INFINITY ? 0.f : top;
-            float sum = 0.f;
-#pragma unroll 4
-            for (int b = 0; b < blocks; ++b) {
-              if (!has(b)) continue;
-              const float2 ml = __ldcg(&A.part_ml[row_at(b) + q]);
-              sum = fmaf(ml.y, exp2_approx(ml.x - zero), sum);
-            }
-            sh.ml[q] = make_float2(zero, sum == 0.f ? 0.f : 1.f / sum);
-            if (A.lse) {
-              const int rr = r0 + q;
-              A.lse[(span.first + rr / A.G) * static_cast<int64_t>(A.H_q) + pc.h * A.G + rr % A.G] =
-                  (top + log2f(sum)) * 0.693147180559945309f;
-            }
-          }
-          if (!meet()) break;
-          constexpr int kAt = 8;  // elements of a thread on the way at once
-          for (int x0 = threadIdx.x; x0 < n_rows * (D / 4); x0 += 256 * kAt) {
-            float4 acc[kAt];
-#pragma unroll
-            for (int e = 0; e < kAt; ++e) acc[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-            for (int b = 0; b < blocks; ++b) {
-              float4 v[kAt];
-              float f[kAt];
-#pragma unroll
-              for (int e = 0; e < kAt; ++e) {
-                v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-                f[e] = -INFINITY;
-                if (has(b)) {
-                  const int x = min(x0 + 256 * e, n_rows * (D / 4) - 1);
-                  const int64_t at = row_at(b) + x / (D / 4);
-                  v[e] = __ldcg(reinterpret_cast<const float4*>(A.part_o + at * D + x % (D / 4) * 4));
-                  f[e] = __ldcg(&A.part_ml[at]).x;
-                }
-              }
-#pragma unroll
-              for (int e = 0; e < kAt; ++e) {
-                const int x = min(x0 + 256 * e, n_rows * (D / 4) - 1);
-                const float2 zi = sh.ml[x / (D / 4)];
-                const float g = exp2_approx(f[e] - zi.x) * zi.y;
-                acc[e].x = fmaf(v[e].x, g, acc[e].x);
-                acc[e].y = fmaf(v[e].y, g, acc[e].y);
-                acc[e].z = fmaf(v[e].z, g, acc[e].z);
-                acc[e].w = fmaf(v[e].w, g, acc[e].w);
-              }
-            }
-#pragma unroll
-            for (int e = 0; e < kAt; ++e) {
-              const int x = x0 + 256 * e;
-              if (x < n_rows * (D / 4)) {
-                const int rr = r0 + x / (D / 4);
-                __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(A.out) +
-                                     (span.first + rr / A.G) * A.o_row + (pc.h * A.G + rr % A.G) * A.o_head + x % (D / 4) * 4;
-                *reinterpret_cast<uint2*>(dst) =
-                    make_uint2(pack_bf16(acc[e].x, acc[e].y), pack_bf16(acc[e].z, acc[e].w));
-              }
-            }
-          }
-        }
-        if (!meet()) break;  // sh.last is read
-      }
       piece_done(k);
       if (!more) break;
     }
@@ -1014,6 +941,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int64_t x0 = x, x1 = cta < n_cta ? begin(cta + 1) : total;
       int k = 0;
       int64_t base = 0;  // cost before the group of sequences
+      if (split && lane == 0) reinterpret_cast<Cut*>(A.cuts)[cta].n_rows = 0;
       while (ok) {
         if (k > 1 && !wait(sh.piece_empty[k & 1], ((k >> 1) + 1) & 1)) break;
         Piece& pc = sh.piece[k & 1];
@@ -1055,7 +983,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int kv_end = seen(span, A.causal, (r0 + n_rows - 1) / A.G);
           const int all = (kv_end + kTile - 1) / kTile;
           steps = max(all, 1);
-          const int p0 = cut(x, w0, w, steps), p1 = cut(min(x1, w1), w0, w, steps);
+          const int p0 = cut(x, w0, w, steps, split), p1 = cut(min(x1, w1), w0, w, steps, split);
           slot = 2 * cta + (x == x0 ? 0 : 1);
           x = w1;
           if (p0 >= p1) continue;
@@ -1077,23 +1005,30 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) mbar_arrive(smem_addr(&sh.piece_full[k & 1]));
         if (!found) break;
         // Who else is at the unit: read after the next piece has been announced.
+        Cut* const cut_here = reinterpret_cast<Cut*>(A.cuts) + cta;
         const int c0 = w0 >= x0 ? cta : shares.block_of(w0), c1 = w1 <= x1 ? cta : shares.block_of(w1 - 1);
         int pieces = 1;
         if (c0 != c1) {
           pieces = 0;
+          int at = -1;  // the first block with a piece
 #pragma unroll 1
           for (int c = c0; c <= c1; c += 32) {
             const int64_t from = max(begin(c + lane), w0), to = min(begin(c + lane + 1), w1);
-            const unsigned has =
-                __ballot_sync(0xffffffffu, c + lane <= c1 && cut(from, w0, w, steps) < cut(to, w0, w, steps));
-            if (lane == 0) sh.mask[k & 1][(c - c0) / 32] = has;
+            const unsigned has = __ballot_sync(
+                0xffffffffu, c + lane <= c1 && cut(from, w0, w, steps, split) < cut(to, w0, w, steps, split));
+            if (at < 0 && has) at = c + __ffs(has) - 1;
+            if (at == cta && lane == 0) cut_here->mask[(c - c0) / 32] = has;
             pieces += __popc(has);
+          }
+          if (pieces > 1 && at == cta && lane == 0) {
+            for (int b = 0; b < (cta - c0) / 32; ++b) cut_here->mask[b] = 0;
+            cut_here->n_rows = pc.n_rows, cut_here->first = pc.first, cut_here->r0 = pc.r0, cut_here->h = pc.h;
+            cut_here->c0 = c0, cut_here->blocks = c1 - c0 + 1;
+            cut_here->slot0 = 2 * c0 + (begin(c0) == w0 ? 0 : 1);
           }
         }
         if (lane == 0) {
           pc.n_pieces = pieces;
-          pc.c0 = c0, pc.c1 = c1;
-          pc.slot0 = 2 * c0 + (begin(c0) == w0 ? 0 : 1);
           pc.slot = slot;
         }
         __syncwarp();
@@ -1105,6 +1040,93 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 12) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, 512);
+  }
+}
+
+// Joins the pieces of the units that were cut: a block takes 32 rows of one, a warp
+// four at a time, eight pieces of each on the way at once.  (The last block at a
+// unit did it before: 15 us behind the others, beside their traffic.)
+template <int D>
+__global__ void __launch_bounds__(256) attend_join_units_kernel(const AttendArgs A) {
+  depend_wait();
+  depend_launch();
+  const Cut& cu = reinterpret_cast<const Cut*>(A.cuts)[blockIdx.x];
+  const int n_rows = cu.n_rows, blocks = cu.blocks, r0 = cu.r0;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int q0 = blockIdx.y * 32 + 4 * warp;
+  if (q0 >= n_rows) return;
+  auto has = [&](int b) { return b < blocks && (cu.mask[b >> 5] >> (b & 31) & 1); };
+  auto row_at = [&](int b) { return static_cast<int64_t>(b ? 2 * (cu.c0 + b) : cu.slot0) * (2 * kTile); };
+  constexpr int kVec = D / 32;  // channels of a lane
+  // lane (r, b): piece b (b + 8, ...) of row q0 + r
+  const int qr = min(q0 + (lane >> 3), n_rows - 1);
+  auto stat = [&](int b) { return has(b) ? __ldcg(&A.part_ml[row_at(b) + qr]) : make_float2(-INFINITY, 0.f); };
+  float top = -INFINITY, sum = 0.f;
+  for (int b0 = 0; b0 < blocks; b0 += 8) top = fmaxf(top, stat(b0 + (lane & 7)).x);
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const float zero = top == -INFINITY ? 0.f : top;
+  float acc[4][kVec];
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) acc[r][e] = 0.f;
+  for (int b0 = 0; b0 < blocks; b0 += 8) {
+    float v[4][8][kVec];
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+      const bool there = has(b0 + b);
+      const float* src = A.part_o + (row_at(b0 + b) + q0) * D + lane * kVec;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[r][b][e] = 0.f;
+        if (there && q0 + r < n_rows) {
+          if constexpr (kVec == 4) {
+            const float4 u = __ldcg(reinterpret_cast<const float4*>(src + r * D));
+            v[r][b][0] = u.x, v[r][b][1] = u.y, v[r][b][2] = u.z, v[r][b][3] = u.w;
+          } else {
+            const float2 u = __ldcg(reinterpret_cast<const float2*>(src + r * D));
+            v[r][b][0] = u.x, v[r][b][1] = u.y;
+          }
+        }
+      }
+    }
+    const float2 ml = stat(b0 + (lane & 7));
+    const float f = exp2_approx(ml.x - zero);
+    sum = fmaf(ml.y, f, sum);
+#pragma unroll
+    for (int b = 0; b < 8; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float g = __shfl_sync(0xffffffffu, f, 8 * r + b);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) acc[r][e] = fmaf(v[r][b][e], g, acc[r][e]);
+      }
+  }
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  auto where = [&](int r) {  // row r of the unit among the tokens and heads
+    const int rr = r0 + r, t = rr / A.G;
+    return make_int2(cu.first + t, cu.h * A.G + rr - t * A.G);
+  };
+  if (A.lse && (lane & 7) == 0 && q0 + (lane >> 3) < n_rows) {
+    const int2 at = where(qr);
+    A.lse[static_cast<int64_t>(at.x) * A.H_q + at.y] = (top + log2f(sum)) * 0.693147180559945309f;
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const float w = __shfl_sync(0xffffffffu, inv, 8 * r);
+    if (q0 + r < n_rows) {
+      const int2 at = where(q0 + r);
+      __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(A.out) + at.x * A.o_row + at.y * A.o_head + lane * kVec;
+      if constexpr (kVec == 4)
+        *reinterpret_cast<uint2*>(dst) =
+            make_uint2(pack_bf16(acc[r][0] * w, acc[r][1] * w), pack_bf16(acc[r][2] * w, acc[r][3] * w));
+      else
+        *reinterpret_cast<uint32_t*>(dst) = pack_bf16(acc[r][0] * w, acc[r][1] * w);
+    }
   }
 }
 
@@ -1146,7 +1168,7 @@ hf_status cache_map(CUtensorMap* map, const CacheArgs& c, const void* base, int 
 }
 
 template <int SRC, int D>
-hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int box, cudaStream_t stream) {
+hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int max_kv, int box, cudaStream_t stream) {
   CUtensorMap maps[2] = {};
   if constexpr (SRC == kByTensorCopies) {
     for (int v = 0; v < 2; ++v) {
@@ -1158,30 +1180,37 @@ hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int box, cudaStr
   constexpr int kBytes = Smem<SRC, D>::kRest + static_cast<int>(sizeof(Shared<Smem<SRC, D>::kStages>));
   HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes),
               "hf_attend: shared memory size");
-  HF_CUDA_TRY(launch_dependent(kern, dim3(std::min(device_sm_count(), kMaxBlocks)), dim3(kThreads), kBytes, stream,
-                               maps[0], maps[1], c, a, box),
+  // units of fewer steps are never cut: without longer ones there is nothing to join
+  const int split = max_kv >= 2 * kLeastSteps * kTile;
+  const unsigned blocks = std::min(device_sm_count(), kMaxBlocks);
+  HF_CUDA_TRY(launch_dependent(kern, dim3(blocks), dim3(kThreads), kBytes, stream, maps[0], maps[1], c, a, box, split),
               "hf_attend: launch");
+  if (split)
+    HF_CUDA_TRY(launch_dependent(attend_join_units_kernel<D>, dim3(blocks, 2 * kTile / 32), dim3(256), 0, stream, a),
+                "hf_attend: joining launch");
   return HF_OK;
 }
 
 template <int D>
-hf_status attend_tiles_d(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, cudaStream_t stream) {
-  if (kind == HF_CACHE_Q4) return launch_tiles<kFromCodes, D>(c, a, 0, stream);
+hf_status attend_tiles_d(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_kv, cudaStream_t stream) {
+  if (kind == HF_CACHE_Q4) return launch_tiles<kFromCodes, D>(c, a, max_kv, 0, stream);
   // rows that lie together: a page's, in pieces that divide a step
   int box = kTile;
   while (c.table && c.block_size % box) box /= 2;
-  if (box < 8 || c.rows == 0) return launch_tiles<kByCpAsync, D>(c, a, 0, stream);
-  return launch_tiles<kByTensorCopies, D>(c, a, box, stream);
+  if (box < 8 || c.rows == 0) return launch_tiles<kByCpAsync, D>(c, a, max_kv, 0, stream);
+  return launch_tiles<kByTensorCopies, D>(c, a, max_kv, box, stream);
 }
 
 }  // namespace
+
+size_t attend_cuts_bytes() { return kMaxBlocks * sizeof(Cut); }
 
 bool attend_tiles_takes(hf_cache_kind kind, hf_dtype dtype, int D) {
   return dtype == HF_BF16 && kind != HF_CACHE_F32 && (D == 64 || D == 128);
 }
 
-hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, cudaStream_t stream) {
-  return c.D == 64 ? attend_tiles_d<64>(c, a, kind, stream) : attend_tiles_d<128>(c, a, kind, stream);
+hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_kv, cudaStream_t stream) {
+  return c.D == 64 ? attend_tiles_d<64>(c, a, kind, max_kv, stream) : attend_tiles_d<128>(c, a, kind, max_kv, stream);
 }
 
 }  // namespace hf
