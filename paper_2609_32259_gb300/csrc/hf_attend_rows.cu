@@ -233,9 +233,13 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
     const int64_t row_bytes = kQ4 ? D / 2 : C.row_stride * 2;
     const char* ksb = C.ks + static_cast<int64_t>(h) * C.rows * (D / 16);
     const char* vsb = C.vs + static_cast<int64_t>(h) * C.rows * (D / 16);
-    auto row_of = [&](int step) -> int {  // of key `lane` of this warp's step
-      const int key = step * R::kStep + warp * KB + lane;
-      return step < p1 && lane < KB && key < kv_end ? cache_row(C, seq, key) : -1;
+    // of key `lane` of this warp's step; its entry is loaded a step before it is used
+    auto there = [&](int step) { return step < p1 && lane < KB && step * R::kStep + warp * KB + lane < kv_end; };
+    auto entry_of = [&](int step) {
+      return there(step) ? cache_entry(C, seq, step * R::kStep + warp * KB + lane) : 0;
+    };
+    auto row_of = [&](int step, int entry) {
+      return there(step) ? cache_row_of(C, step * R::kStep + warp * KB + lane, entry) : -1;
     };
     auto issue = [&](int step, int stage, int row) {
       if (step < p1) {
@@ -259,12 +263,13 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
       cp_async_commit();
     };
 
-    int rows[S];  // looked up side by side
+    int entries[S];
 #pragma unroll
-    for (int i = 0; i < S; ++i) rows[i] = row_of(p0 + i);
+    for (int i = 0; i < S; ++i) entries[i] = entry_of(p0 + i);
 #pragma unroll
-    for (int i = 0; i < S - 1; ++i) issue(p0 + i, i, rows[i]);
-    int row = rows[S - 1];
+    for (int i = 0; i < S - 1; ++i) issue(p0 + i, i, row_of(p0 + i, entries[i]));
+    int entry = entries[S - 1];
+
     // ---- queries
     uint32_t qf[NT][D / 16][2];
     float q_off[kQ4 ? NT : 1][kQ4 ? NG : 1][2];
@@ -344,8 +349,8 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
     for (int step = p0; step < p1; ++step) {
       cp_async_wait<S - 2>();
       __syncwarp();  // the stage is everybody's, and the one before it is read
-      issue(step + S - 1, ahead, row);
-      row = row_of(step + S);
+      issue(step + S - 1, ahead, row_of(step + S - 1, entry));
+      entry = entry_of(step + S);
       const uint32_t st = ring_a + stage * R::kStage;
       if (++stage == S) stage = 0;
       if (++ahead == S) ahead = 0;

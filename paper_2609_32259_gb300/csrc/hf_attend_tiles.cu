@@ -678,18 +678,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int seq = piece_at(k).seq, h = piece_at(k).h, t0 = piece_at(k).t0, n_ops = piece_at(k).n_ops,
                   kv_end = piece_at(k).kv_end;
         piece_done(k);
-        auto row_of = [&](int j, int key) {  // of key `key` of step j
+        // Row of key `key` of step j; its entry is loaded a step before it is used.
+        auto entry_of = [&](int j, int key) {
           key += (t0 + j) * kTile;
-          return j < n_ops && key < kv_end ? cache_row(C, seq, key) : -1;
+          return j < n_ops && key < kv_end ? cache_entry(C, seq, key) : 0;
+        };
+        auto row_of = [&](int j, int key, int entry) {
+          key += (t0 + j) * kTile;
+          return j < n_ops && key < kv_end ? cache_row_of(C, key, entry) : -1;
         };
         if constexpr (SRC == kByTensorCopies) {
           // Lane b + nb * c: channels 64 c .. of the rows b * box .. of a step.
           const int nb = kTile / box, piece = lane % nb, part = lane / nb;
           const bool active = part < D / 64;
-          int ahead = active ? row_of(0, piece * box) : -1;
+          int entry = entry_of(0, piece * box);
           for (int j = 0; j < n_ops && ok; ++j) {
-            const int row = ahead;
-            ahead = active ? row_of(j + 1, piece * box) : -1;
+            const int row = active ? row_of(j, piece * box, entry) : -1;
+            entry = entry_of(j + 1, piece * box);
             const int key0 = (t0 + j) * kTile;
             const unsigned there = __ballot_sync(0xffffffffu, row >= 0);
             const bool bad = there != __ballot_sync(0xffffffffu, active && key0 + piece * box < kv_end);
@@ -726,7 +731,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                                    C.vs + static_cast<int64_t>(h) * C.rows * (D / 16)};
           Q4Words<D> q[4];
           const int m = lane & 3;
-          int row = row_of(0, 32 * w + lane), later = row_of(1, 32 * w + lane);
+          const int key = 32 * w + lane;
+          int row = row_of(0, key, entry_of(0, key)), entry = entry_of(1, key);
 #pragma unroll
           for (int p = 0; p < 4; ++p)
             load_q4<D>(q[p], codes[0], scales[0], __shfl_sync(0xffffffffu, row, 8 * p + (lane >> 2)), m);
@@ -734,8 +740,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!wait(sh.empty[stage], phase)) break;
             const uint32_t base = smem_addr(smem) + M::kKV + stage * M::kOperand;
             if (x & 1) {
-              row = later;
-              later = row_of((x >> 1) + 2, 32 * w + lane);
+              row = row_of((x >> 1) + 1, key, entry);
+              entry = entry_of((x >> 1) + 2, key);
             }
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
@@ -756,7 +762,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int x = 0; x <= 2 * n_ops; ++x) {
             if (x < 2 * n_ops) {
               if (!wait(sh.empty[stage], phase)) break;
-              if ((x & 1) == 0) row = row_of(x >> 1, 32 * w + lane);
+              if ((x & 1) == 0) row = row_of(x >> 1, 32 * w + lane, entry_of(x >> 1, 32 * w + lane));
               const char* src = x & 1 ? vb : kb;
               const uint32_t base = smem_addr(smem) + M::kKV + stage * M::kOperand;
 #pragma unroll 4

@@ -52,34 +52,38 @@ __device__ __forceinline__ int64_t cache_capacity(const CacheArgs& c, int s) {
 }
 
 // Row of the buffers that holds row t >= 0 of sequence s, or -1 (and a status
-// bit) where there is none.
-__device__ __forceinline__ int cache_row(const CacheArgs& c, int s, int64_t t) {
+// bit) where there is none: in two steps, so that the load of the first may be
+// under way while its caller does other things.
+__device__ __forceinline__ int cache_block(const CacheArgs& C, int64_t t) {
+  return static_cast<int>(C.block_shift >= 0 ? t >> C.block_shift : t / C.block_size);
+}
+__device__ __forceinline__ int cache_entry(const CacheArgs& c, int s, int64_t t) {
+  if (!c.table) return c.row0 ? c.row0[s] : 0;
+  return c.table[static_cast<int64_t>(s) * c.max_blocks + min(cache_block(c, t), c.max_blocks - 1)];
+}
+__device__ __forceinline__ int cache_row_of(const CacheArgs& c, int64_t t, int entry) {
   if (c.table) {
-    int b, r;
-    if (c.block_shift >= 0) {
-      b = static_cast<int>(t >> c.block_shift);
-      r = static_cast<int>(t) & (c.block_size - 1);
-    } else {
-      b = static_cast<int>(t / c.block_size);
-      r = static_cast<int>(t - static_cast<int64_t>(b) * c.block_size);
-    }
+    const int b = cache_block(c, t);
     if (b >= c.max_blocks) {
       set_status(c, HF_CHECK_CAPACITY);
       return -1;
     }
-    const int64_t row = static_cast<int64_t>(c.table[static_cast<int64_t>(s) * c.max_blocks + b]) * c.block_size;
+    const int64_t row = static_cast<int64_t>(entry) * c.block_size;
     if (row < 0 || row + c.block_size > c.rows) {
       set_status(c, HF_CHECK_BAD_BLOCK);
       return -1;
     }
-    return static_cast<int>(row) + r;
+    return static_cast<int>(row + (t - static_cast<int64_t>(b) * c.block_size));
   }
-  const int64_t row = (c.row0 ? c.row0[s] : 0) + t;
+  const int64_t row = entry + t;
   if (row < 0 || row >= c.rows) {
     set_status(c, HF_CHECK_CAPACITY);
     return -1;
   }
   return static_cast<int>(row);
+}
+__device__ __forceinline__ int cache_row(const CacheArgs& c, int s, int64_t t) {
+  return cache_row_of(c, t, cache_entry(c, s, t));
 }
 
 // The sequence of packed token `tok`, found by a whole warp: the number of
