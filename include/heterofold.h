@@ -519,11 +519,11 @@ typedef struct {
   const void* d_v;
   int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
   /* Optional: the tokens' queries, normed and rotated like the keys into
-     d_q_out (d_q itself, or not overlapping it), the same strides. */
+     d_q_out (d_q itself with the same strides, or not overlapping it). */
   int32_t H_q;
   const void* d_q;
   void* d_q_out;
-  int64_t q_row_stride, q_head_stride;
+  int64_t q_row_stride, q_head_stride, q_out_row_stride, q_out_head_stride;
   /* Optional rotation of keys and queries, rotate-half pairs (i, i + D/2):
      cos and sin of every position [rope_len][D/2][2] (hf_rope_table).  The
      position of a token is its row in the sequence plus d_pos0[s]. */

@@ -97,6 +97,7 @@ class AppendDesc(ctypes.Structure):
         ("v_row_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64),
         ("H_q", ctypes.c_int32), ("d_q", _p), ("d_q_out", _p),
         ("q_row_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+        ("q_out_row_stride", ctypes.c_int64), ("q_out_head_stride", ctypes.c_int64),
         ("d_rope", _p), ("rope_len", ctypes.c_int32), ("d_pos0", _p),
         ("d_k_norm", _p), ("d_q_norm", _p), ("eps", ctypes.c_float),
     ]

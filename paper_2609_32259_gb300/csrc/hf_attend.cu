@@ -385,10 +385,13 @@ extern "C" hf_status hf_attend(const hf_cache* cache, const hf_attend_desc* d, v
   a.cuts = a.part_ml + part_rows(device_sm_count());
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
   const int max_kv = static_cast<int>(std::min<int64_t>(d->max_kv_len, c.rows));
+  // Up to 16 query rows of a KV head are two of the other form's columns; from
+  // there on tiles of 128 rows, with the tensor core's own operand paths.
   const int64_t max_rows = static_cast<int64_t>(std::min(d->max_q_len, d->n_tok)) * a.G;
-  if (attend_rows_takes(cache->kind, d->dtype, c.D) && max_rows <= 16)
+  if (c.rows > 0 && attend_rows_takes(cache->kind, d->dtype, c.D) && max_rows <= 16)
     return attend_rows(c, a, cache->kind, static_cast<int>(max_rows), stream);
-  if (attend_tiles_takes(cache->kind, d->dtype, c.D)) return attend_tiles(c, a, cache->kind, max_kv, stream);
+  if (c.rows > 0 && attend_tiles_takes(cache->kind, d->dtype, c.D))
+    return attend_tiles(c, a, cache->kind, max_kv, stream);
   switch (c.D) {
     case 32: return attend_general<32>(c, a, cache->kind, d->dtype, max_kv, stream);
     case 64: return attend_general<64>(c, a, cache->kind, d->dtype, max_kv, stream);

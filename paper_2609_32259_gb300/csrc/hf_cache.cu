@@ -92,7 +92,7 @@ struct AppendArgs {
   const char* v;
   const char* q;
   char* q_out;
-  int64_t k_row, k_head, v_row, v_head, q_row, q_head;
+  int64_t k_row, k_head, v_row, v_head, q_row, q_head, qo_row, qo_head;
   const float* rope;
   const int32_t* pos0;
   const float* k_norm;
@@ -266,18 +266,19 @@ struct Places {
   // positions differ: d_pos0); -1 and a status bit where there is none.
   __device__ __forceinline__ int row(const CacheArgs& C, const TokenArgs& t, const int32_t* d_pos0, int tok,
                                      int64_t* pos) const {
-    int seq, f, s, p;
+    int seq, f, s, p, e;
     if (C.n_seq <= 32) {
       seq = __popc(__ballot_sync(0xffffffffu, end <= tok));
+      e = __shfl_sync(0xffffffffu, end, seq & 31);
       f = __shfl_sync(0xffffffffu, first, seq & 31);
       s = __shfl_sync(0xffffffffu, start, seq & 31);
       p = __shfl_sync(0xffffffffu, pos0, seq & 31);
     } else {
       seq = sequence_of(t.tok_ptr, C.n_seq, tok);
       const int at = min(seq, C.n_seq - 1);
-      f = t.tok_ptr[at], s = t.start[at], p = d_pos0 ? d_pos0[at] : 0;
+      f = t.tok_ptr[at], e = t.tok_ptr[at + 1], s = t.start[at], p = d_pos0 ? d_pos0[at] : 0;
     }
-    if (seq >= C.n_seq || f > tok || f < 0) {
+    if (seq >= C.n_seq || f > tok || f < 0 || e <= tok) {
       set_status(C, HF_CHECK_BAD_OFFSETS);
       return -1;
     }
@@ -426,7 +427,7 @@ __global__ void __launch_bounds__(32 * kWarps, D <= 128 ? 4 : 1) append_kernel(c
         }
       }
       if (live && role == 2) {
-        T* dst = reinterpret_cast<T*>(A.q_out) + tok * A.q_row + h * A.q_head;
+        T* dst = reinterpret_cast<T*>(A.q_out) + tok * A.qo_row + h * A.qo_head;
 #pragma unroll
         for (int i = 0; i < NC; ++i) store8(dst + 8 * (m + L::kPerHead * i), x[i]);
       }
@@ -646,15 +647,19 @@ extern "C" hf_status hf_cache_append(const hf_cache* cache, const hf_append_desc
   a.k_row = d->k_row_stride, a.k_head = d->k_head_stride;
   a.v_row = d->v_row_stride, a.v_head = d->v_head_stride;
   a.q_row = d->q_row_stride, a.q_head = d->q_head_stride;
+  a.qo_row = d->q_out_row_stride, a.qo_head = d->q_out_head_stride;
   a.H_q = d->d_q ? d->H_q : 0;
   if (d->d_q && (d->H_q < 1 || d->H_q > 65536 || !d->d_q_out)) return bad_argument(who, "queries need H_q >= 1 and d_q_out");
   if (!fill_strides(&a.k_row, &a.k_head, c.H, c.D, es) || !fill_strides(&a.v_row, &a.v_head, c.H, c.D, es) ||
-      !fill_strides(&a.q_row, &a.q_head, std::max(a.H_q, 1), c.D, es))
+      !fill_strides(&a.q_row, &a.q_head, std::max(a.H_q, 1), c.D, es) ||
+      !fill_strides(&a.qo_row, &a.qo_head, std::max(a.H_q, 1), c.D, es))
     return bad_argument(who, "strides must be positive multiples of 16 bytes");
   if ((reinterpret_cast<uintptr_t>(d->d_q) | reinterpret_cast<uintptr_t>(d->d_q_out) |
        reinterpret_cast<uintptr_t>(d->d_rope) | reinterpret_cast<uintptr_t>(d->d_k_norm) |
        reinterpret_cast<uintptr_t>(d->d_q_norm)) & 15u)
     return bad_argument(who, "queries, rotation table and norm weights must be 16-byte aligned");
+  if (d->d_q && d->d_q == d->d_q_out && (a.q_row != a.qo_row || a.q_head != a.qo_head))
+    return bad_argument(who, "queries rotated in place need the same strides");
   if (d->d_rope && d->rope_len < 1) return bad_argument(who, "rope_len must be positive");
   if ((d->d_k_norm || d->d_q_norm) && !(d->eps >= 0.f)) return bad_argument(who, "eps must not be negative");
   if (d->n_tok == 0) return HF_OK;

@@ -261,7 +261,7 @@ class KVCache:
             self.layers = kv.shape[0]
             self.device = kv.device
         self.rows = int(rows)
-        self.block_table, self.row0 = block_table, row0
+        self.block_table, self.block_size, self.row0 = block_table, int(block_size), row0
         self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._workspace = workspace
         max_blocks = 0
@@ -297,7 +297,7 @@ class KVCache:
         rs, hs = _rows("k", k, rows, H, D, k.dtype)
         self.kind, self.H, self.D, self.n_seq, self.layers, self.rows = _NAMES[k.dtype], H, D, n_seq, 1, rows
         self.kv, self.codes, self.scales, self.device = (k, v), None, None, k.device
-        self.block_table, self.row0 = None, row0
+        self.block_table, self.block_size, self.row0 = None, 0, row0
         self._status = torch.zeros(1, dtype=torch.int32, device=k.device)
         self._workspace = workspace
         if row0 is not None:
@@ -330,14 +330,13 @@ class KVCache:
         n, n_seq, H, D, dt = k.shape[0], self.n_seq, self.H, self.D, k.dtype
         k_row, k_head = _rows("k", k, n, H, D, dt)
         v_row, v_head = _rows("v", v, n, H, D, dt)
-        H_q = d_q = d_q_out = q_row = q_head = 0
+        H_q = d_q = d_q_out = q_row = q_head = qo_row = qo_head = 0
         if q is not None:
             if q_out is None:
                 raise ValueError("q needs q_out")
             H_q = q.shape[1]
             q_row, q_head = _rows("q", q, n, H_q, D, dt)
-            if _rows("q_out", q_out, n, H_q, D, dt) != (q_row, q_head):
-                raise ValueError("q and q_out must have the same strides")
+            qo_row, qo_head = _rows("q_out", q_out, n, H_q, D, dt)
             d_q, d_q_out = q.data_ptr(), q_out.data_ptr()
         d_rope = rope_len = 0
         if rope is not None:
@@ -352,7 +351,7 @@ class KVCache:
             self._descs[layer],
             B.AppendDesc(_CODES[dt], n, _ints("tok_ptr", tok_ptr, n_seq + 1), _ints("start", start, n_seq),
                          k.data_ptr(), v.data_ptr(), k_row, k_head, v_row, v_head, H_q, d_q, d_q_out, q_row, q_head,
-                         d_rope, rope_len, None if pos0 is None else _ints("pos0", pos0, n_seq),
+                         qo_row, qo_head, d_rope, rope_len, None if pos0 is None else _ints("pos0", pos0, n_seq),
                          None if k_norm is None else k_norm.data_ptr(),
                          None if q_norm is None else q_norm.data_ptr(), eps),
             _stream_of(k, stream))

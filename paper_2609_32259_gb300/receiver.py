@@ -1,0 +1,168 @@
+"""A receiver that goes on from a transferred cache: the question's tokens and the
+answer's, layer by layer, behind contexts that hf_transfer wrote.
+
+ReceiverSteps holds what one forward step of a receiver model needs of its
+attention layers: for every layer the model hands in the step's packed queries,
+keys and values (before norm and rotation) and gets its attention outputs back;
+the cache, the lengths and the rotation are kept here.
+
+    python -m paper_2609_32259_gb300.receiver [--q4] [--tokens 4096] [--steps 16]
+
+runs a transfer between two of the paper's model shapes on synthetic inputs, a
+question and some decoding steps (random projections stand in for the receiver's
+own weights), optionally with the transferred cache packed into 4 bits, and prints
+what they take.
+"""
+
+from __future__ import annotations
+
+import argparse
+from typing import Optional, Sequence
+
+import numpy as np
+import torch
+
+from . import pipeline
+
+
+class ReceiverSteps:
+    """Attention of a receiver's next tokens over its cache.
+
+    cache   KVCache whose sequences have room behind their rows
+    lens    rows of every sequence that are there (host), e.g. the contexts'
+    rope    cos and sin of every position to come (pipeline.rope_table)
+    """
+
+    def __init__(self, cache: pipeline.KVCache, lens: Sequence[int], rope: torch.Tensor,
+                 k_norm: Optional[torch.Tensor] = None, q_norm: Optional[torch.Tensor] = None, eps: float = 1e-6):
+        self.cache, self.rope, self.k_norm, self.q_norm, self.eps = cache, rope, k_norm, q_norm, eps
+        self.lens = np.asarray(lens, np.int32)
+        if self.lens.shape != (cache.n_seq,):
+            raise ValueError(f"lens must have {cache.n_seq} values")
+        self._new = None
+
+    def begin(self, new: Sequence[int]) -> None:
+        """A step of new[s] tokens of every sequence s (0: none)."""
+        new = np.asarray(new, np.int32)
+        if new.shape != self.lens.shape or (new < 0).any():
+            raise ValueError("one count of new tokens a sequence, none negative")
+        if int((self.lens + new).max()) > self.rope.shape[0]:
+            raise ValueError("the rotation table ends before these positions")
+        dev = self.cache.device
+        ints = np.concatenate([[0], np.cumsum(new), self.lens, self.lens + new]).astype(np.int32)
+        at = torch.as_tensor(ints).to(dev)
+        n = len(new)
+        self._new = new
+        self.tok_ptr, self.start, self.kv_len = at[:n + 1], at[n + 1:2 * n + 1], at[2 * n + 1:]
+
+    def layer(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The step's tokens in one layer: keys and values [n_tok, H, D] behind the
+        others, attention of queries [n_tok, H_q, D] over all of them."""
+        if self._new is None:
+            raise ValueError("begin() comes first")
+        rotated = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        self.cache.append(layer, k, v, self.tok_ptr, self.start, rope=self.rope, q=q, q_out=rotated,
+                          k_norm=self.k_norm, q_norm=self.q_norm, eps=self.eps)
+        out = torch.empty_like(rotated) if out is None else out
+        self.cache.attend(layer, rotated, out, self.tok_ptr, self.kv_len, max_q_len=int(self._new.max()),
+                          max_kv_len=int((self.lens + self._new).max()))
+        return out
+
+    def end(self) -> None:
+        """The step's tokens are part of the sequences."""
+        self.lens = self.lens + self._new
+        self._new = None
+
+
+def packed_in_4_bits(cache: pipeline.KVCache, lens: Sequence[int]) -> pipeline.KVCache:
+    """The first lens[s] rows of every sequence, all layers, in a 4-bit cache with
+    the same rows and pages."""
+    q4 = pipeline.KVCache(kind="q4", H=cache.H, D=cache.D, n_seq=cache.n_seq, rows=cache.rows, layers=cache.layers,
+                          block_table=cache.block_table, block_size=cache.block_size, row0=cache.row0,
+                          device=cache.device)
+    ptr = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    tok_ptr = torch.as_tensor(ptr).to(cache.device)
+    start = torch.zeros(cache.n_seq, dtype=torch.int32, device=cache.device)
+    dtype = cache.kv.dtype
+    k, v = (torch.empty((int(ptr[-1]), cache.H, cache.D), dtype=dtype, device=cache.device) for _ in range(2))
+    for l in range(cache.layers):
+        cache.read(l, k, v, tok_ptr, start)
+        q4.append(l, k, v, tok_ptr, start)
+    return q4
+
+
+def _paged_job(direction, n_new: int, device):
+    """A transfer of `direction` into a paged cache with room for n_new tokens more."""
+    from . import workloads as W
+
+    w = direction.with_(paged=True)
+    tok = W.tokens(w)
+    T, b = int(tok.T_r), w.block_size
+    need = -(-(T + n_new) // b)
+    rng = np.random.default_rng(w.seed)
+    table = rng.permutation(need).astype(np.int32)[None]
+    sender = W.sender_kv(w, tok.T_s, device)
+    Wm, bias, r = W.maps(w, device)
+
+    class Paged:
+        block_table, n_blocks = table, need
+
+    return w, T, pipeline.job_from_workload(w, tok, sender, Wm, bias, r, paged=Paged, device=device)
+
+
+def main() -> None:
+    from . import workloads as W
+
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    ap.add_argument("--tokens", type=int, default=4096, help="receiver tokens of the context")
+    ap.add_argument("--question", type=int, default=48)
+    ap.add_argument("--steps", type=int, default=16)
+    ap.add_argument("--group", type=int, default=7, help="query heads a KV head")
+    ap.add_argument("--q4", action="store_true", help="pack the transferred cache into 4 bits")
+    a = ap.parse_args()
+    dev = torch.device("cuda")
+    w, T, job = _paged_job(W.llama_to_qwen25(a.tokens), a.question + a.steps, dev)
+    job.step()
+    cache = pipeline.KVCache.of_job(job)
+    if a.q4:
+        cache = packed_in_4_bits(cache, [T])
+    rope = pipeline.rope_table(T + a.question + a.steps, w.D_r, theta=w.theta_r, device=dev)
+    rec = ReceiverSteps(cache, [T], rope)
+    g = torch.Generator(device=dev).manual_seed(1)
+    heads = w.H_r * (a.group + 2)
+    proj = torch.randn((w.H_r * a.group * w.D_r, heads * w.D_r), generator=g, device=dev, dtype=torch.bfloat16)
+    proj *= proj.shape[0] ** -0.5
+    x = torch.randn((a.question, proj.shape[0]), generator=g, device=dev, dtype=torch.bfloat16)
+    torch.nn.functional.rms_norm(x @ proj, (proj.shape[1],))  # the libraries load here
+
+    def forward(x):
+        rec.begin([x.shape[0]])
+        for l in range(w.L_r):
+            qkv = (x @ proj).view(x.shape[0], heads, w.D_r)
+            n = w.H_r * a.group
+            o = rec.layer(l, qkv[:, :n], qkv[:, n:n + w.H_r], qkv[:, n + w.H_r:])
+            x = torch.nn.functional.rms_norm(o.reshape(x.shape[0], -1), (proj.shape[0],))
+        rec.end()
+        return x
+
+    def timed(what, fn):
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        y = fn()
+        e1.record()
+        torch.cuda.synchronize()
+        print("%-40s %8.3f ms" % (what, e0.elapsed_time(e1)))
+        return y
+
+    kind = "4-bit" if a.q4 else "bf16"
+    y = timed("question: %d tokens, %d layers, %s cache" % (a.question, w.L_r, kind), lambda: forward(x))
+    for i in range(a.steps):
+        y = forward(y[-1:]) if i < a.steps - 1 else timed("the last of %d decoding steps" % a.steps,
+                                                          lambda: forward(y[-1:]))
+    assert cache.status() == 0 and torch.isfinite(y.float()).all()
+    print("context %d tokens, now %d rows a layer" % (T, int(rec.lens[0])))
+
+
+if __name__ == "__main__":
+    main()

@@ -59,6 +59,7 @@ def test_null_descriptors(B):
     dict(d_v=None), dict(d_k=4104), dict(k_row_stride=100), dict(v_head_stride=4), dict(d_q=64, H_q=0, d_q_out=64),
     dict(d_q=64, H_q=4), dict(d_q=72, H_q=4, d_q_out=64), dict(d_rope=64, rope_len=0), dict(d_rope=68, rope_len=5),
     dict(d_k_norm=64, eps=-1.0), dict(d_k_norm=64, eps=float("nan")), dict(d_q=64, d_q_out=64, H_q=4, q_row_stride=3),
+    dict(d_q=64, d_q_out=128, H_q=4, q_out_head_stride=-64), dict(d_q=64, d_q_out=64, H_q=4, q_out_row_stride=512),
 ])
 def test_appends(B, over):
     kw = dict(dtype=0, n_tok=5, d_tok_ptr=64, d_start=64, d_k=4096, d_v=4096)

@@ -297,3 +297,21 @@ def test_attend_streams_and_graphs(kind, n):
     graph.replay()
     torch.cuda.synchronize()
     s.check(out2, None)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "q4"])
+@pytest.mark.parametrize("n", [1, 40])
+def test_attend_empty_cache(kind, n):
+    c = pipeline.KVCache(kind=kind, H=2, D=64, n_seq=1, rows=0)
+    q = torch.ones((n, 4, 64), dtype=TDT["f32" if kind == "f32" else "bf16"], device="cuda")
+    out, lse = torch.full_like(q, 3.0), torch.zeros((n, 4), device="cuda")
+    c.attend(0, q, out, _i32([0, n]), _i32([0]), lse=lse)
+    assert (out == 0).all() and torch.isneginf(lse).all() and c.status() == 0
+
+
+@pytest.mark.parametrize("kind", ["bf16", "q4"])
+def test_attend_many_units_and_cuts(kind):
+    # long enough that shares end inside units, at every kind of place
+    for lens in ([(300, 4000), (1, 9000), (64, 2500)], [(40, 20000)], [(3, 3000)] * 7, [(2000, 2000), (0, 0), (129, 6000)]):
+        s = Setup(kind, 2, 8, 64, lens, block=16, seed=len(lens))
+        s.check(*s.run())
