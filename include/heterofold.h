@@ -604,8 +604,8 @@ typedef struct {
  * bytes must be zero before the first call and are zero after every call; one
  * call at a time may use it.  At most two launches; n_tok 0 does nothing.
  * A non-finite value in a row that a query sees reaches its output as it does in
- * fp32 sums; one in a row past kv_len never does, and one in a row that a causal
- * query does not see may, where another query of its call sees that row.
+ * fp32 sums; one in a row that it does not see (past kv_len, or after a causal
+ * query) never does.
  */
 #define HF_ATTEND_ZEROED 65536
 hf_status hf_attend_workspace_size(const hf_cache* cache, size_t* bytes);

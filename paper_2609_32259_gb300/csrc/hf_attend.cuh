@@ -130,6 +130,61 @@ __device__ __forceinline__ float from_float<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// This lane's D / 32 channels of a cache row's head in fp32.
+template <int KIND, int D>
+__device__ __forceinline__ void lane_channels(const CacheArgs& C, bool value, int64_t row, int h, float* x) {
+  constexpr int N = D / 32;
+  const int c0 = (threadIdx.x & 31) * N;
+  if constexpr (KIND == HF_CACHE_Q4) {
+    static_assert(N == 2 || N == 4, "a lane's codes are one byte or two");
+    const int64_t at = h * C.rows + row;
+    const int g = c0 / 32;
+    const char* p = (value ? C.v : C.k) + at * (D / 2) + (D / 8 * (c0 % 32 / 4) + 4 * g + c0 % 4) / 2;
+    const uint32_t w = N == 4 ? *reinterpret_cast<const uint16_t*>(p) : *reinterpret_cast<const uint8_t*>(p);
+    const uint32_t s = reinterpret_cast<const uint16_t*>((value ? C.vs : C.ks) + at * (D / 16))[g];
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      x[e] = __uint_as_float(s << 16) * static_cast<float>(static_cast<int>(w >> (4 * e) & 15u) - 8);
+  } else {
+    const char* p = (value ? C.v : C.k) + (row * C.row_stride + h * C.head_stride + c0) * 2;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      x[e] = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[e]);
+  }
+}
+
+// The outputs of query q over its keys [k0, k1) again, by a warp: adds to a lane's
+// D / 32 channels of them, unnormalised for the maximum m.  For the tensor-core forms,
+// where an infinity or NaN in a row that q does not see, but another query of its
+// tile does, has met q's probability of zero.
+template <int KIND, int D>
+__device__ __forceinline__ void outputs_again(const CacheArgs& C, const AttendArgs& A, int seq, int h,
+                                              const __nv_bfloat16* q, int k0, int k1, float m, float* o) {
+  constexpr int N = D / 32;
+  const float base = m == -INFINITY ? 0.f : m;
+  float x[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) x[e] = __bfloat162float(q[(threadIdx.x & 31) * N + e]);
+#pragma unroll 1
+  for (int key = k0; key < k1; ++key) {
+    const int row = cache_row(C, seq, key);
+    float k[N], v[N], dot = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) k[e] = v[e] = 0.f;
+    if (row >= 0) {
+      lane_channels<KIND, D>(C, false, row, h, k);
+      lane_channels<KIND, D>(C, true, row, h, v);
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) dot = fmaf(x[e], k[e], dot);
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, w);
+    const float p = exp2f(fmaf(dot, A.scale_log2, -base));
+#pragma unroll
+    for (int e = 0; e < N; ++e) o[e] = fmaf(p, v[e], o[e]);
+  }
+}
+
 // The form for few query rows a KV head (hf_attend_rows.cu): bf16 queries, bf16
 // and 4-bit caches, D 64 and 128.  max_rows: tokens times G at most.
 bool attend_rows_takes(hf_cache_kind kind, hf_dtype dtype, int D);

@@ -550,6 +550,30 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
         }
       }
     }
+    if (kv_end > all_see) {  // some row does not see some key
+      __syncwarp();
+      for (int q = 0; q < n_rows; ++q) {
+        constexpr int N = D / 32;
+        float* dst = so + q * kOut + lane * N;
+        bool bad = false;
+#pragma unroll
+        for (int e = 0; e < N; ++e) bad |= !isfinite(dst[e]);
+        if (!__any_sync(0xffffffffu, bad)) continue;
+        const int rr = r0 + q, end = seen(span, A.causal, rr / A.G);
+        const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(A.q) +
+                                   static_cast<int64_t>(span.first + rr / A.G) * A.q_row +
+                                   (h * A.G + rr % A.G) * A.q_head;
+        float again[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) again[e] = 0.f;
+        for (int step = p0; step < p1; ++step) {
+          const int key = step * R::kStep + warp * KB;
+          outputs_again<KIND, D>(C, A, seq, h, src, key, min(key + KB, end), s_m[warp][q], again);
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) dst[e] = again[e];
+      }
+    }
     __syncthreads();
 
     const bool whole = p0 == 0 && p1 == steps;

@@ -567,6 +567,54 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) break;
       if (more_q) q_there();  // its first scores come while the outputs go
+      // Where a row does not see some of its steps' keys: see outputs_again.
+      const int end = min(dual ? key0 - kTile : key0, span.kv);
+      if (__any_sync(0xffffffffu, live && n > 0 && lim < end)) {
+        uint64_t zeros = 0;  // or NaN
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          tmem_ld32(to + c, o);
+          tmem_ld_wait32(o);
+#pragma unroll
+          for (int e = 0; e < 32; e += 2)
+            zeros = fma2(pack2(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), 0, zeros);
+        }
+        float sum, more_sum;
+        unpack2(zeros, &sum, &more_sum);
+        sum += more_sum;
+        unsigned bad = __ballot_sync(0xffffffffu, live && !(sum == 0.f));
+        while (bad) {
+          const int who = __ffs(bad) - 1;
+          bad &= bad - 1;
+          constexpr int N = D / 32;
+          float again[N];
+#pragma unroll
+          for (int e = 0; e < N; ++e) again[e] = 0.f;
+          const int upto = __shfl_sync(0xffffffffu, lim, who);
+          const int64_t tok = span.first + __shfl_sync(0xffffffffu, token, who);
+          const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(A.q) + tok * A.q_row +
+                                   (pc.h * A.G + __shfl_sync(0xffffffffu, head, who)) * A.q_head;
+          for (int j = 0; j < n; ++j) {
+            const int key = (pc.t0 + (dual ? 2 * j + i : j)) * kTile;
+            outputs_again<SRC == kFromCodes ? HF_CACHE_Q4 : HF_CACHE_BF16, D>(
+                C, A, pc.seq, pc.h, q, key, min(key + kTile, upto), __shfl_sync(0xffffffffu, m, who), again);
+          }
+#pragma unroll
+          for (int c = 0; c < D; c += 16) {
+            uint32_t o[16];
+            tmem_load_16(to + c, o);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float x = __shfl_sync(0xffffffffu, again[(c + e) % N], (c + e) / N);
+              const int at = SRC == kFromCodes ? (e & 8) + code_place(e & 7) : e;
+              if (lane == who) o[at] = __float_as_uint(x);
+            }
+            tmem_st16(to + c, o);
+          }
+          tmem_st_wait();
+        }
+      }
       if (dual) {
         // the same rows: tile 1's outputs go into tile 0's
         if (i == 1) {

@@ -255,6 +255,35 @@ def test_attend_non_finite_rows(n):
     assert ((out[n:].double() - o).abs() <= P.bound(o, absv, size, s.dtype)).all()
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("kind,D,lens", [
+    ("bf16", 64, [(4, 300), (2, 5)]), ("bf16", 128, [(3, 2000)]), ("q4", 64, [(4, 300)]), ("q4", 128, [(3, 2000)]),
+    ("bf16", 64, [(70, 300), (33, 20)]), ("bf16", 128, [(200, 3000), (1, 64)]), ("bf16", 128, [(300, 300)]),
+    ("q4", 64, [(200, 900)]), ("q4", 128, [(30, 4000)]), ("f32", 64, [(40, 100)]), ("bf16", 96, [(40, 100)])])
+def test_attend_non_finite_rows_after_a_query(kind, D, lens, bad):
+    # the last rows hold an infinity or NaN in a key's and a value's channel: queries
+    # before them come out as if they were not there, the last ones with them
+    s = Setup(kind, 2, 4, D, lens, block=16, seed=D)
+    ends = np.cumsum([n for n, _ in lens])
+    for rows in s.rows_of:
+        at = rows[len(rows) - 1]
+        if kind == "q4":
+            s.cache.scales[0, :, 1, at, 0] = bad
+        else:
+            s.val[:, at, 1, 3] = bad
+    out, _ = s.run(lse=False)
+    first = 0
+    for (n, m), rows, end in zip(s.lens, s.rows_of, ends):
+        n1 = n - 1
+        if n1 > 0:
+            k, v = s.val[0, rows[:m - 1]], s.val[1, rows[:m - 1]]
+            o, _, absv, size = P.attend(s.q[first:first + n1], k, v, True)
+            assert ((out[first:first + n1].double() - o).abs() <= P.bound(o, absv, size, s.dtype)).all()
+        assert torch.isfinite(out[end - 1, :4].float()).all() and torch.isnan(out[end - 1, 4:].float()).any()
+        first = int(end)
+    assert s.cache.status() == 0
+
+
 @pytest.mark.parametrize("n", [1, 40])
 def test_attend_rows_past_32_bit_offsets(n):
     # a pool of 2.4 million rows: the last rows lie past 2^31 elements and 2^32 bytes
