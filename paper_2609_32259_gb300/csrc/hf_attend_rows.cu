@@ -23,8 +23,9 @@
 // operations for two codes.  Queries are scaled by 2^64 (and 2^60), and group
 // scales apply to the 32-channel partial scores in fp32; for the values they and
 // 2^64 go into P (one rounding, the one that P takes anyway).  The offset of 8 is the
-// score accumulator's start, -8 sum(q), and a further product with a constant
-// row for the values.
+// score accumulator's start, -8 sum(q); from the values' codes it is taken before
+// the product: where the weights fall on codes of 8, a difference of sums would leave
+// their rounding.
 #include <algorithm>
 
 #include "hf_attend.cuh"
@@ -82,6 +83,11 @@ __device__ __forceinline__ float exp2_approx(float x) {
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t sub_bf16(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 v =
+      __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 __device__ __forceinline__ float bf16_half(uint32_t w, int which) {
@@ -324,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
     const float inv_scale = 1.f / scale;
     const int all_see = seen(span, A.causal, r0 / A.G);  // by the first row, so by all
 
-    float o[NT][D / 16][4], o_off[kQ4 ? NT : 1][kQ4 ? NG : 1][4];
+    float o[NT][D / 16][4];
     // m: the maximum, scaled; reach: the largest score that moves nothing; neg: what
     // is added to a scaled score before the power
     float m[NT][2], l[NT][2], reach[NT][2], neg[NT][2];
@@ -334,12 +340,6 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
       for (int i = 0; i < D / 16; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
-      if constexpr (kQ4) {
-#pragma unroll
-        for (int i = 0; i < NG; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o_off[nt][i][e] = 0.f;
-      }
       m[nt][0] = m[nt][1] = reach[nt][0] = reach[nt][1] = -INFINITY;
       neg[nt][0] = neg[nt][1] = 0.f;
       l[nt][0] = l[nt][1] = 0.f;
@@ -452,13 +452,6 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
                 o[nt][i][e] *= fix;
                 o[nt][i][e + 2] *= fix;
               }
-              if constexpr (kQ4) {
-#pragma unroll
-                for (int i = 0; i < NG; ++i) {
-                  o_off[nt][i][e] *= fix;
-                  o_off[nt][i][e + 2] *= fix;
-                }
-              }
             }
         }
 #pragma unroll
@@ -482,15 +475,19 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
             const float f0 = bf16_half(vs[0][gr / 2], gr & 1), f1 = bf16_half(vs[1][gr / 2], gr & 1);
             const uint32_t c8 = __byte_perm(w[0][gr / 2], w[1][gr / 2], gr & 1 ? 0x7632 : 0x5410);
             const uint32_t e8 = __byte_perm(w[2][gr / 2], w[3][gr / 2], gr & 1 ? 0x7632 : 0x5410);
-            const uint32_t d8 = c8 >> 8, g8 = e8 >> 8;
+            const uint32_t at[4] = {c8, c8 >> 8, e8, e8 >> 8};
+            uint32_t lo[4], hi[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              lo[i] = sub_bf16(at[i] & 0x000f000fu, 0x00080008u);
+              hi[i] = sub_bf16(at[i] & 0x00f000f0u, 0x00800080u);
+            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               const uint32_t b0 = movmatrix_trans(pack_bf16(s[nt][0] * f0, s[nt][1] * f0));
               const uint32_t b1 = movmatrix_trans(pack_bf16(s[nt][2] * f1, s[nt][3] * f1));
-              mma16816(o[nt][2 * gr], c8 & 0x000f000fu, d8 & 0x000f000fu, e8 & 0x000f000fu, g8 & 0x000f000fu, b0, b1);
-              mma16816(o[nt][2 * gr + 1], c8 & 0x00f000f0u, d8 & 0x00f000f0u, e8 & 0x00f000f0u, g8 & 0x00f000f0u, b0,
-                       b1);
-              mma16816(o_off[nt][gr], 0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u, b0, b1);
+              mma16816(o[nt][2 * gr], lo[0], lo[1], lo[2], lo[3], b0, b1);
+              mma16816(o[nt][2 * gr + 1], hi[0], hi[1], hi[2], hi[3], b0, b1);
             }
           }
         } else {
@@ -535,11 +532,10 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
           const float back = 590295810358705651712.f;  // 2^69
 #pragma unroll
           for (int gr = 0; gr < NG; ++gr) {
-            const float off = o_off[nt][gr][e];
-            dst[32 * gr + 4 * g] = (o[nt][2 * gr][e] - off) * back;
-            dst[32 * gr + 4 * g + 2] = (o[nt][2 * gr][e + 2] - off) * back;
-            dst[32 * gr + 4 * g + 1] = (o[nt][2 * gr + 1][e] * 0.0625f - off) * back;
-            dst[32 * gr + 4 * g + 3] = (o[nt][2 * gr + 1][e + 2] * 0.0625f - off) * back;
+            dst[32 * gr + 4 * g] = o[nt][2 * gr][e] * back;
+            dst[32 * gr + 4 * g + 2] = o[nt][2 * gr][e + 2] * back;
+            dst[32 * gr + 4 * g + 1] = o[nt][2 * gr + 1][e] * (0.0625f * back);
+            dst[32 * gr + 4 * g + 3] = o[nt][2 * gr + 1][e + 2] * (0.0625f * back);
           }
         } else {
 #pragma unroll

@@ -196,6 +196,16 @@ def test_attend_scale_and_large_scores(kind):
     s.check(*s.run())
 
 
+@pytest.mark.parametrize("kind", ["bf16", "q4"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attend_few_rows_large_scores(kind, D):
+    # nearly all weight on one key: channels whose code stands for zero are sums of the others'
+    s = Setup(kind, 1, 4, D, [(1, 400), (2, 160), (1, 3000)], block=16, seed=8)
+    for f in (8, -1):
+        s.q.mul_(f)
+        s.check(*s.run())
+
+
 @pytest.mark.parametrize("n", [1, 2, 70, 200])
 def test_attend_strided_projections(n):
     # q, k, v as slices of one projection's output, outputs into a slice
