@@ -385,10 +385,18 @@ extern "C" hf_status hf_attend(const hf_cache* cache, const hf_attend_desc* d, v
   a.cuts = a.part_ml + part_rows(device_sm_count());
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
   const int max_kv = static_cast<int>(std::min<int64_t>(d->max_kv_len, c.rows));
-  // Up to 16 query rows of a KV head are two of the other form's columns; from
-  // there on tiles of 128 rows, with the tensor core's own operand paths.
+  // Up to 16 query rows of a KV head are two columns of the form for few rows.  One
+  // sequence's few heads take up to 128 in chunks of 16 rows there, which read the keys
+  // again but start on all SMs at once, while the tiles leave most idle.  Measured (us,
+  // few rows / tiles; 8 KV heads of 128 channels, bf16): one sequence, 64 rows, 200 keys
+  // 17 / 17, 1,000 keys 19 / 27, 4,000 keys 31 / 37; 128 rows, 4,000 keys 40 / 38.
+  // 16 rows of 4 sequences of 4,000 keys 35 / 42, 32 rows 42 / 43, of 16,000 keys
+  // 105 / 76; 4-bit, the same 36 / 44, 42 / 45, 76 / 81.
   const int64_t max_rows = static_cast<int64_t>(std::min(d->max_q_len, d->n_tok)) * a.G;
-  if (c.rows > 0 && attend_rows_takes(cache->kind, d->dtype, c.D) && max_rows <= 16)
+  const int64_t reads = (max_rows + 15) / 16 * c.n_seq * c.H * static_cast<int64_t>(max_kv);
+  const bool few =
+      max_rows <= 16 || (max_rows <= 128 && c.n_seq * static_cast<int64_t>(c.H) <= 8 && reads <= 128 * 1024);
+  if (few && c.rows > 0 && attend_rows_takes(cache->kind, d->dtype, c.D))
     return attend_rows(c, a, cache->kind, static_cast<int>(max_rows), stream);
   if (c.rows > 0 && attend_tiles_takes(cache->kind, d->dtype, c.D))
     return attend_tiles(c, a, cache->kind, max_kv, stream);

@@ -164,6 +164,15 @@ def test_attend_prompts(kind, D, n, m):
     s.check(*s.run())
 
 
+@pytest.mark.parametrize("kind", ["bf16", "q4"])
+@pytest.mark.parametrize("n,m", [(5, 900), (16, 16), (16, 2000), (32, 1100), (32, 10), (33, 500)])
+def test_attend_one_sequence_of_few_heads(kind, n, m):
+    # both sides of the rule that takes these as few rows: up to 128 rows of a KV head
+    s = Setup(kind, 2, 4, 128, [(n, m)], block=16, seed=n)
+    s.check(*s.run())
+    s.check(*s.run(causal=False), causal=False)
+
+
 def test_attend_long_prompt():
     s = Setup("bf16", 1, 4, 128, [(3000, 3000), (1, 5000), (700, 2100)], block=32, seed=5)
     s.check(*s.run())
