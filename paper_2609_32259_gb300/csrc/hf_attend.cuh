@@ -192,8 +192,10 @@ hf_status attend_rows(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kin
 
 // The form for many query rows (hf_attend_tiles.cu): the same types and widths.
 bool attend_tiles_takes(hf_cache_kind kind, hf_dtype dtype, int D);
-// max_kv: where it is short, sequences are not split.
-hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_kv, cudaStream_t stream);
+// max_rows: tokens times G at most of a sequence; from it and max_kv follows whether
+// units are cut.
+hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int64_t max_rows, int max_kv,
+                       cudaStream_t stream);
 size_t attend_cuts_bytes();  // of AttendArgs::cuts
 
 // Joins `ns` parts of every (token, query head), [part][token][head].

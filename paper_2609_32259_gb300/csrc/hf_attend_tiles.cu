@@ -8,8 +8,9 @@
 // one's softmax runs under the other's products.  With at most 128 rows both tiles
 // are the same rows and take every other step.  One block an SM stays for the
 // whole call: the units' costs are shared out evenly, so long prompts end
-// together and the keys of a few short questions are split over all SMs; units
-// that were cut are joined by a kernel that follows.
+// together and the keys of a few short questions are split over all SMs.  Units
+// that were cut are joined by a kernel that follows; where whole ones come out nearly
+// even none is cut.
 //
 //   warps 0-3, 4-7  queries and softmax of tile 0 and 1: a thread a row.  Scores come from
 //                   tensor memory, probabilities go back there as bf16 over them,
@@ -33,6 +34,13 @@
 // products of one tile follow each other in issue order, so a tile's new scores
 // also say that its last product with V is done.
 //
+// Measured (L2 flushed; of the burst's 1,939 TFLOP/s): a prompt of 8,192 tokens, 8 KV
+// and 32 query heads of 128 channels 385-390 us (1,420 TFLOP/s, 73%: exponentials beside
+// the products); six prompts of 314 to 1,558 tokens 69 us (some 20,000 cycles before
+// the first and after the last product); four questions of 20 to 34 tokens behind 4,704
+// to 27,628 77 us, of 27 to 71 over 4-bit caches 91 us (expanding an operand of
+// 128 keys takes a loader 1,400 cycles).
+//
 // Every wait is bounded; one that runs out sets HF_CHECK_TIMEOUT and ends the
 // block.
 #include <algorithm>
@@ -46,7 +54,7 @@ namespace hf {
 namespace {
 
 constexpr int kTile = 128;       // query rows of a tile, keys of a step
-constexpr int kThreads = 512;    // 13 warps work; registers are shared out by warpgroup
+constexpr int kThreads = 512;    // registers are shared out by warpgroup
 constexpr float kStretch = 8.f;  // log2 of what a score may pass the running maximum by
 
 __device__ __forceinline__ void cp_async_16_or_zero(uint32_t dst, const void* src, bool there) {
@@ -250,8 +258,7 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* map, int32
 // Who does what
 // ---------------------------------------------------------------------------
 // A unit is 256 query rows of one KV head, its cost about its keys: visible keys
-// times G, plus 256 G (what starting and ending one takes, two steps of 128
-// keys).  Within a head the costs grow linearly with the unit (causal), so sums
+// times G, plus those of kOwnSteps steps of 128.  Within a head the costs grow linearly with the unit (causal), so sums
 // of them have a closed form.  All units' costs, laid end to end, are shared out
 // evenly over the blocks; a share's ends fall inside units, which are cut there
 // at whole steps.
@@ -279,7 +286,9 @@ struct Cut {
   uint32_t mask[kMaxBlocks / 32];  // blocks c0 + i that have a piece
 };
 
-constexpr int kOwnSteps = 4;  // what starting and ending a unit takes, in steps
+// What starting and ending a unit takes, in steps (1 / 4 / 8: six prompts of up to 1,558
+// tokens 83 / 74 / 80 us, one of 8,192 437 / 390 / 395, with cut units).
+constexpr int kOwnSteps = 4;
 struct UnitCost {
   int64_t w0, dw, head;  // cost of unit 0, its growth, all units of one head
   int tiles;
@@ -296,8 +305,10 @@ __device__ __forceinline__ UnitCost unit_cost(const SeqSpan& s, const AttendArgs
 
 // Cuts of a unit with cost [w0, w0 + w) and n steps: the step where cost x lies.
 // A piece of less than kLeastSteps goes to its neighbour; without `split` units
-// stay whole.
-constexpr int kLeastSteps = 6;
+// stay whole.  (2 / 4 / 6 / 12: questions behind 4,704 to 27,628 keys 77 / 77 / 81 / 88 us.)
+constexpr int kLeastSteps = 4;
+constexpr int kLongSteps = 12;  // no unit of fewer is cut where all have fewer
+constexpr int kCutSteps = 20;   // what cutting costs a block
 __device__ __forceinline__ int cut(int64_t x, int64_t w0, int64_t w, int n, int split) {
   if (x <= w0) return 0;
   if (x >= w0 + w) return n;
@@ -1222,7 +1233,8 @@ hf_status cache_map(CUtensorMap* map, const CacheArgs& c, const void* base, int 
 }
 
 template <int SRC, int D>
-hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int max_kv, int box, cudaStream_t stream) {
+hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int64_t max_rows, int max_kv, int box,
+                       cudaStream_t stream) {
   CUtensorMap maps[2] = {};
   if constexpr (SRC == kByTensorCopies) {
     for (int v = 0; v < 2; ++v) {
@@ -1234,9 +1246,18 @@ hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int max_kv, int 
   constexpr int kBytes = Smem<SRC, D>::kRest + static_cast<int>(sizeof(Shared<Smem<SRC, D>::kStages>));
   HF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes),
               "hf_attend: shared memory size");
-  // units of fewer steps are never cut: without longer ones there is nothing to join
-  const int split = max_kv >= 2 * kLeastSteps * kTile;
+  // Cutting units costs what kCutSteps steps take: partial results of up to 128 KB a
+  // piece go through memory, and are joined.  Whole units leave blocks with more steps
+  // than others: by up to a unit, less what its last round lacks.  (us, cut / whole, 8 KV
+  // and 32 query heads: a prompt of 2,000 tokens 53 / 51, three 112 / 105, one of 8,192
+  // 382 / 396; 64 queries behind 2,000 keys, 32 sequences 82 / 67; 300 behind 4,000, 8
+  // sequences 140 / 151.)
   const unsigned blocks = std::min(device_sm_count(), kMaxBlocks);
+  const int64_t unit = 2 * kTile, rows = static_cast<int64_t>(a.n_tok) * a.G;
+  const int64_t units = std::min(c.n_seq * ((max_rows + unit - 1) / unit), rows / unit + c.n_seq) * c.H;
+  const int64_t steps = (max_kv + kTile - 1) / kTile, rounds = (units + blocks - 1) / blocks;
+  const bool even = steps <= 32 && (rounds * blocks - units) * (steps + kOwnSteps) <= kCutSteps * static_cast<int64_t>(blocks);
+  const int split = steps >= kLongSteps && !even;
   HF_CUDA_TRY(launch_dependent(kern, dim3(blocks), dim3(kThreads), kBytes, stream, maps[0], maps[1], c, a, box, split),
               "hf_attend: launch");
   if (split)
@@ -1246,13 +1267,14 @@ hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int max_kv, int 
 }
 
 template <int D>
-hf_status attend_tiles_d(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_kv, cudaStream_t stream) {
-  if (kind == HF_CACHE_Q4) return launch_tiles<kFromCodes, D>(c, a, max_kv, 0, stream);
+hf_status attend_tiles_d(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int64_t max_rows, int max_kv,
+                         cudaStream_t stream) {
+  if (kind == HF_CACHE_Q4) return launch_tiles<kFromCodes, D>(c, a, max_rows, max_kv, 0, stream);
   // rows that lie together: a page's, in pieces that divide a step
   int box = kTile;
   while (c.table && c.block_size % box) box /= 2;
-  if (box < 8 || c.rows == 0) return launch_tiles<kByCpAsync, D>(c, a, max_kv, 0, stream);
-  return launch_tiles<kByTensorCopies, D>(c, a, max_kv, box, stream);
+  if (box < 8 || c.rows == 0) return launch_tiles<kByCpAsync, D>(c, a, max_rows, max_kv, 0, stream);
+  return launch_tiles<kByTensorCopies, D>(c, a, max_rows, max_kv, box, stream);
 }
 
 }  // namespace
@@ -1263,8 +1285,10 @@ bool attend_tiles_takes(hf_cache_kind kind, hf_dtype dtype, int D) {
   return dtype == HF_BF16 && kind != HF_CACHE_F32 && (D == 64 || D == 128);
 }
 
-hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int max_kv, cudaStream_t stream) {
-  return c.D == 64 ? attend_tiles_d<64>(c, a, kind, max_kv, stream) : attend_tiles_d<128>(c, a, kind, max_kv, stream);
+hf_status attend_tiles(const CacheArgs& c, const AttendArgs& a, hf_cache_kind kind, int64_t max_rows, int max_kv,
+                       cudaStream_t stream) {
+  return c.D == 64 ? attend_tiles_d<64>(c, a, kind, max_rows, max_kv, stream)
+                   : attend_tiles_d<128>(c, a, kind, max_rows, max_kv, stream);
 }
 
 }  // namespace hf
