@@ -14,9 +14,10 @@
 //   S^T [keys x queries] = K Q^T,   O^T [channels x queries] += V^T P^T,
 // so that eight queries fill its columns (M = 16 rows are keys or channels,
 // never padding), K comes as it lies and V transposed by ldmatrix, and P^T turns
-// from one layout to the other in two movmatrix.  A row's maximum moves only
-// when a score passes it by 2^8: until then sums stay below 2^8 of their
-// largest term, and most steps need one vote and no shuffle.
+// from one layout to the other in two movmatrix.  A row's maximum moves with every
+// larger score: the largest weight is 1 then, and exact when it is rounded to bf16, which
+// matters where it has most of the sum (one row's outputs have no others to average
+// with).  Most steps need one vote and no shuffle all the same.
 //
 // 4-bit rows stay codes: the nibbles c of a word are masked in place and are, as
 // bf16 numbers, c 2^-133 and 16 c 2^-133 (subnormal, exact), one or two
@@ -30,7 +31,7 @@
 // Measured (L2 flushed; of the copy's 6.79 TB/s): 32 sequences of 500 to 16,384 keys,
 // 4 KV heads, 28 query heads 50 us (4.7 TB/s, 69%: the loop runs at the memory's rate,
 // starting and ending pieces takes the rest); one of 1,000 keys, 8 and 32 heads 9.4 us
-// (latency); four 4-bit contexts of 131,072 keys 152 us (4.0 TB/s, 59%: some 360
+// (latency); four 4-bit contexts of 131,072 keys 150 us (4.0 TB/s, 59%: some 360
 // instructions for 16 keys, the issue slots half full, the integer pipe just above that).
 #include <algorithm>
 
@@ -41,7 +42,6 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr float kStretch = 8.f;  // log2 of what a score may pass the running maximum by
 
 __device__ __forceinline__ void cp_async_16_or_zero(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -362,11 +362,12 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
       if (++ahead == S) ahead = 0;
       const int key0 = step * R::kStep + warp * KB;
       if (key0 >= kv_end) continue;
+      constexpr int NB = KB / 16;  // blocks of 16 keys: their chains run side by side
+      float scores[NB][NT][4];
 #pragma unroll
       for (int b = 0; b < KB / 16; ++b) {
         // scores
-        float s[NT][4];
-        uint32_t vs[2][kQ4 ? (NG + 1) / 2 : 1];  // scales of the values of keys kappa(g), kappa(g + 8)
+        float (&s)[NT][4] = scores[b];
         if constexpr (kQ4) {
           uint32_t w[2][NG], sc[2][(NG + 1) / 2];
 #pragma unroll
@@ -377,7 +378,6 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
             else
               lds_words<2>(st + chunk_at<KIND, D>(key, t >> 1) + 8 * (t & 1), w[e]);
             lds_words<NG / 2>(st + R::kKs + key * R::kScale, sc[e]);
-            lds_words<NG / 2>(st + R::kVs + key * R::kScale, vs[e]);
           }
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
@@ -424,51 +424,70 @@ __global__ void __launch_bounds__(kThreads, (kBlocks<KIND, NT>))
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[nt][e] += s2[nt][e];
         }
-        // what is not seen, and the running maximum (of scores before scaling)
-        const int ka = key0 + 16 * b + (kQ4 ? kappa(g) : g), kb8 = ka + 8;
-        bool past = false;
-        if (key0 + 16 * b + 16 > all_see) {
+      }
+      // what is not seen, and the running maximum (of scores before scaling)
+      if (key0 + KB > all_see) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const int ka = key0 + 16 * b + (kQ4 ? kappa(g) : g), kb8 = ka + 8;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if ((e < 2 ? ka : kb8) >= lim[nt][e & 1]) s[nt][e] = -INFINITY;
+              if ((e < 2 ? ka : kb8) >= lim[nt][e & 1]) scores[b][nt][e] = -INFINITY;
         }
+      }
+      bool past = false;
+      float tops[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float top = fmaxf(scores[0][nt][e], scores[0][nt][e + 2]);
+#pragma unroll
+          for (int b = 1; b < NB; ++b) top = fmaxf(top, fmaxf(scores[b][nt][e], scores[b][nt][e + 2]));
+          tops[nt][e] = top;
+          past |= top > reach[nt][e];
+        }
+      if (__any_sync(0xffffffffu, past)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) past |= fmaxf(s[nt][e], s[nt][e + 2]) > reach[nt][e];
-        if (__any_sync(0xffffffffu, past)) {
+          for (int e = 0; e < 2; ++e) {
+            float top = tops[nt][e];
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+            const float next = fmaxf(m[nt][e], top * scale);
+            const float fix = next == -INFINITY ? 1.f : exp2_approx(m[nt][e] - next);
+            m[nt][e] = next;
+            reach[nt][e] = next == -INFINITY ? next : next * inv_scale;
+            neg[nt][e] = next == -INFINITY ? 0.f : kShift - next;
+            l[nt][e] *= fix;
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float top = fmaxf(s[nt][e], s[nt][e + 2]);
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-              const float next = fmaxf(m[nt][e], top * scale);
-              const float fix = next == -INFINITY ? 1.f : exp2_approx(m[nt][e] - next);
-              m[nt][e] = next;
-              reach[nt][e] = next == -INFINITY ? next : (next + kStretch) * inv_scale;
-              neg[nt][e] = next == -INFINITY ? 0.f : kShift - next;
-              l[nt][e] *= fix;
-#pragma unroll
-              for (int i = 0; i < D / 16; ++i) {
-                o[nt][i][e] *= fix;
-                o[nt][i][e + 2] *= fix;
-              }
+            for (int i = 0; i < D / 16; ++i) {
+              o[nt][i][e] *= fix;
+              o[nt][i][e + 2] *= fix;
             }
-        }
+          }
+      }
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            s[nt][e] = exp2_approx(fmaf(s[nt][e], scale, neg[nt][e & 1]));
-            l[nt][e & 1] += s[nt][e];
+            scores[b][nt][e] = exp2_approx(fmaf(scores[b][nt][e], scale, neg[nt][e & 1]));
+            l[nt][e & 1] += scores[b][nt][e];
           }
-        // outputs
+      // outputs
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const float (&s)[NT][4] = scores[b];
         if constexpr (kQ4) {
+          uint32_t vs[2][(NG + 1) / 2];  // scales of the values of keys kappa(g), kappa(g + 8)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) lds_words<NG / 2>(st + R::kVs + (16 * b + kappa(g + 8 * e)) * R::kScale, vs[e]);
           uint32_t w[4][(NG + 1) / 2];
 #pragma unroll
           for (int e = 0; e < 4; ++e)  // keys t, t + 4, t + 8, t + 12: rows 2 t, 2 t + 1, ... of S^T

@@ -215,6 +215,34 @@ def test_attend_few_rows_large_scores(kind, D):
         s.check(*s.run())
 
 
+@pytest.mark.parametrize("kind", ["bf16", "q4"])
+def test_attend_one_row_keeps_the_largest_weight_exact(kind):
+    # values only behind key j, which has the largest score: the output is its weight
+    # times them, rounded to bf16 (half a unit in the last of 8 places) from fp32 sums
+    # (scores of at most 40 in 64 products: 2^-23 * 64 * 40; 2^-11 of it in all)
+    m, D = 30000, 64
+    s = Setup(kind, 2, 4, D, [(1, m)], block=16, seed=11)
+    rows = s.rows_of[0]
+    for j in (500, 10007, 15064, 20001, 29990):
+        s.val[1] = 0
+        if kind == "q4":
+            s.cache.codes[0, 1] = 0x88
+            c = torch.randint(1, 16, (2, D), generator=torch.Generator().manual_seed(j))
+            scale = s.cache.scales[0, 1, :, rows[j]].float().cpu()  # [H, D / 32]
+            s.val[1, rows[j]] = ((c - 8) * scale.repeat_interleave(32, -1)).to(s.val)
+            s.cache.codes[0, 1, :, rows[j]] = torch.as_tensor(P.pack_codes(c.numpy().astype(np.uint8))).cuda()
+        else:
+            s.val[1, rows[j]] = torch.randn((2, D), generator=torch.Generator().manual_seed(j)).to(s.val)
+        k = s.val[0, rows[j]].double()  # [H, D]
+        f = torch.tensor([4.7, 5.0, 5.2, 5.5], device="cuda", dtype=torch.double)
+        q = f[None, :, None] * 8 * (k / (k * k).sum(-1, keepdim=True))[:, None]
+        s.q.copy_(q.reshape(1, 8, D).to(s.q.dtype))
+        out, _ = s.run()
+        o, _, _, _ = P.attend(s.q, s.val[0, rows], s.val[1, rows], True)
+        half_unit = 2.0 ** (torch.floor(torch.log2(o.abs())) - 8)
+        assert ((out.double() - o).abs() <= half_unit + 2.0 ** -11 * o.abs()).all(), j
+
+
 @pytest.mark.parametrize("n", [1, 2, 70, 200])
 def test_attend_strided_projections(n):
     # q, k, v as slices of one projection's output, outputs into a slice
