@@ -15,8 +15,8 @@
 //   warps 0-3, 4-7  queries and softmax of tile 0 and 1: a thread a row.  Scores come from
 //                   tensor memory, probabilities go back there as bf16 over them,
 //                   as the next product's first operand.  The running maximum
-//                   moves only when a score passes it by 2^8; the outputs in tensor
-//                   memory are rescaled then, by the same thread.
+//                   may lag by 2^8 in calls of many rows; when it moves, the
+//                   outputs in tensor memory are rescaled, by the same thread.
 //   warps 8-11      loaders, into the 128-byte-swizzled layout.  bf16: one warp
 //                   brings K and V by tensor copies, a lane a piece of a page (a
 //                   step's last rows, where the sequence ends, are cleared: what
@@ -56,9 +56,11 @@ namespace {
 constexpr int kTile = 128;       // query rows of a tile, keys of a step
 constexpr int kThreads = 512;    // registers are shared out by warpgroup
 // log2 of what a score may pass the running maximum by.  (0: one prompt of 8,192 tokens
-// 392 -> 436 us, six prompts 69 -> 79.  A weight that is no power of two is wrong by its
-// rounding to bf16, up to 2^-8 of a row's outputs where one key has most of its sum.)
+// 392 -> 436 us, six prompts 69 -> 79.)  A weight that is no power of two is wrong by its
+// rounding to bf16, up to 2^-8 of a row's outputs where one key has most of its sum:
+// many rows' errors average, calls of few rows have the maximum exact.
 constexpr float kStretch = 8.f;
+constexpr int64_t kFewRows = 2048;
 
 __device__ __forceinline__ void cp_async_16_or_zero(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -525,8 +527,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int e = 0; e < 4; ++e) top4[e] = max3(top4[e], __uint_as_float(s[c + e]), __uint_as_float(s[c + e + 4]));
         const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * A.scale_log2;
-        if (__any_sync(0xffffffffu, top > m + kStretch)) {
-          const float next = top > m + kStretch ? top : m;
+        if (__any_sync(0xffffffffu, top > m + A.stretch)) {
+          const float next = top > m + A.stretch ? top : m;
           const float fix = next == m ? 1.f : exp2_approx(m - next);
           m = next;
           l *= fix;
@@ -1261,7 +1263,9 @@ hf_status launch_tiles(const CacheArgs& c, const AttendArgs& a, int64_t max_rows
   const int64_t steps = (max_kv + kTile - 1) / kTile, rounds = (units + blocks - 1) / blocks;
   const bool even = steps <= 32 && (rounds * blocks - units) * (steps + kOwnSteps) <= kCutSteps * static_cast<int64_t>(blocks);
   const int split = steps >= kLongSteps && !even;
-  HF_CUDA_TRY(launch_dependent(kern, dim3(blocks), dim3(kThreads), kBytes, stream, maps[0], maps[1], c, a, box, split),
+  AttendArgs args = a;
+  args.stretch = static_cast<int64_t>(a.n_tok) * a.H_q <= kFewRows ? 0.f : kStretch;
+  HF_CUDA_TRY(launch_dependent(kern, dim3(blocks), dim3(kThreads), kBytes, stream, maps[0], maps[1], c, args, box, split),
               "hf_attend: launch");
   if (split)
     HF_CUDA_TRY(launch_dependent(attend_join_units_kernel<D>, dim3(blocks, 2 * kTile / 32), dim3(256), 0, stream, a),
